@@ -19,9 +19,11 @@
  *   - "device" pointers are HIP device pointers on the device that was current at rvq_create,
  *     16-byte aligned; the CALLER owns them; the library keeps no reference after the work it
  *     enqueued has run;
+ *   - calls without a context (rvq_rope*, rvq_cache8*) take pointers and a stream of the device that is
+ *     current in the calling thread, and RVQ_EINVAL a stream of another one;
  *   - work is enqueued on the caller's stream (a hipStream_t passed as void*; NULL = the
  *     default stream).  The enqueue calls (rvq_set_codebooks, rvq_get_codebooks, rvq_encode,
- *     rvq_decode*, rvq_pack_codes, rvq_unpack_codes, rvq_ema_update) never allocate, free or
+ *     rvq_decode*, rvq_pack_codes, rvq_unpack_codes, rvq_ema_update, rvq_rope*, rvq_cache8*) never allocate, free or
  *     synchronize; the set-up and diagnostic calls (rvq_create, rvq_destroy, rvq_reserve,
  *     rvq_get_counters, rvq_check_kernels) may do all three;
  *   - the context owns its pre-processed codebook copies and its workspace (all of it allocated
@@ -29,7 +31,7 @@
  *     a context must be used by one host thread and on ONE stream at a time (calls on two
  *     streams would share the workspace and the codebook copies without any ordering); use one
  *     context per stream, or order the streams with events;
- *   - inputs must be finite.  A row with a NaN or an infinity gets unspecified codes (every
+ *   - inputs of the encoder must be finite.  A row with a NaN or an infinity gets unspecified codes (every
  *     code still lies in [0, K) and every access stays in bounds); other rows are unaffected;
  *   - N == 0 / M == 0 is a successful no-op.
  */
@@ -220,6 +222,130 @@ int rvq_attn_decode(rvq_ctx *kctx, rvq_ctx *vctx, const float *dQ, int32_t n_q_h
                     const void *dVCodes, const void *dVStd, int32_t packed, int64_t N,
                     const float *dCos, const float *dSin, float scale, float *dOut,
                     void *dWorkspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Rotary position tables: the angles that rvq_decode_rope, rvq_attn_decode, rvq_rope and the cache of
+ * 8-bit codes below take.  With R = rot channels rotated per head, frequency i < R / 2 is
+ *   theta_i = base^(-2 i / R),
+ * stretched for contexts beyond the orig_len tokens a model was trained on: a frequency that makes
+ * r_i = orig_len theta_i / (2 pi) turns in them keeps a share g_i = clamp((r_i - alpha) / (beta - alpha), 0, 1),
+ *   theta'_i = g_i theta_i + (1 - g_i) theta_i / factor
+ * (interpolation by parts, arXiv 2309.00071; orig_len == 0: g_i = 0, every frequency is divided; factor == 1:
+ * theta'_i = theta_i), and
+ *   dCos[n][i] = amplitude * cos(dPositions[n] theta'_i),  dSin[n][i] likewise,
+ * the angle in 64 bits, rounded once (the angle of position p carries an error of about p 2^-52).
+ *   dPositions  device, int64 [N]
+ *   rot         even, >= 2
+ *   base > 0, factor > 0, orig_len >= 0, amplitude finite; alpha < beta where orig_len > 0
+ *   dCos, dSin  device, float [N][rot / 2]
+ */
+int rvq_rope_tables(const int64_t *dPositions, int64_t N, int32_t rot, double base, double factor,
+                    double orig_len, double alpha, double beta, double amplitude, float *dCos, float *dSin,
+                    void *stream);
+
+enum rvq_rope_layout {
+  RVQ_ROPE_ADJACENT = 0, /* pair i of a head is channels (2 i, 2 i + 1): what rvq_decode_rope rotates   */
+  RVQ_ROPE_HALVES = 1    /* pair i is channels (i, i + rot / 2)                                         */
+};
+
+/*
+ * Rotation of N rows of n_heads head vectors, e.g. of the queries that rvq_attn_decode and rvq_cache8_attn
+ * take: in every head the first rot channels are rotated pair by pair,
+ *   (a, b) -> (a cos[n][i] - b sin[n][i], a sin[n][i] + b cos[n][i]),
+ * in fp32, rounded once; the other channels are copied.
+ *   dX      device, dtype [N][n_heads][head_dim]: row n, head h begins at element n * ldx + h * hsx
+ *   dOut    device, the same with ldo and hso; dOut == dX with equal strides rotates in place, any other
+ *           overlap is not allowed
+ *   rot     even, 2 .. head_dim;  dCos, dSin  device, float [N][rot / 2]
+ * Strides are >= 0 and arbitrary (rows that are aligned to 16 bytes and channels in whole groups of 16
+ * are moved fastest); dX and dOut need the alignment of their elements only.
+ */
+int rvq_rope(const void *dX, int32_t dtype, int64_t N, int32_t n_heads, int32_t head_dim, int32_t rot,
+             int32_t layout, int64_t ldx, int64_t hsx, const float *dCos, const float *dSin, void *dOut,
+             int64_t ldo, int64_t hso, void *stream);
+
+/*
+ * Paged cache of keys and values in 8 bits: the tokens of a sequence that are not (yet) held as RVQ codes.
+ * A page holds RVQ_PAGE_TOKENS tokens of one sequence.  Per page and kv head, one after the other, come
+ *   the keys' codes    uint8 [RVQ_PAGE_TOKENS][head_dim]
+ *   the values' codes  uint8 [head_dim][RVQ_PAGE_TOKENS]     (what a product of weights and values reads)
+ * and, in an array of their own, the scales of the two.  A code is an e4m3 number (4 exponent and 3
+ * mantissa bits, largest 448, no infinity, 0x7f / 0xff NaN), the value is code * scale.  A scale is a power of two:
+ * it places the codes' range and costs them no precision.
+ * The struct is a host-side view; nothing is kept after a call.
+ */
+#define RVQ_PAGE_TOKENS 64
+typedef struct {
+  uint8_t *pages;       /* device, [n_pages][n_kv_heads][2][RVQ_PAGE_TOKENS * head_dim]                  */
+  float *scales;        /* device, [n_pages][n_kv_heads][2]                                             */
+  int64_t n_pages;      /* >= 1                                                                         */
+  int32_t n_kv_heads;   /* 1 .. 1024                                                                    */
+  int32_t head_dim;     /* 64, 128 or 256                                                               */
+  const int32_t *table; /* device, [n_seqs][table_pages]: the pages of every sequence in order.  An entry
+                           outside [0, n_pages) is a page that is not there: its tokens are not written, not
+                           seen by attention, and read as 0                                             */
+  int32_t table_pages;  /* >= 1; a sequence's tokens from table_pages * RVQ_PAGE_TOKENS on have no page    */
+  int32_t n_seqs;       /* 1 .. 65535                                                                   */
+  const int32_t *lengths; /* device, [n_seqs]: tokens of every sequence, those of the current step included */
+} rvq_cache8;
+
+/*
+ * Append: row cu[b] + i of the step (i < n_b = cu[b + 1] - cu[b]) is the token of sequence b at position
+ * lengths[b] - n_b + i.  Its keys are rotated as by rvq_rope (in fp32, no rounding before the code), its values taken as
+ * they are, and both are stored as the nearest codes, ties to even.  Scale of a (page, head, keys or values): the
+ * smallest power of two >= 2^-100 with which every new finite element is within the codes' range, and at least
+ * the page's old scale where the sequence's earlier tokens are in the page already (slot 0 is not among the new
+ * tokens); where it grows, those tokens' codes are rounded again to the new scale.  NaN and infinities are stored as NaN and do
+ * not enter the scale.  Other slots and pages stay as they were.
+ *   dK, dV    device, dtype [rows][n_kv_heads][head_dim], 16-byte aligned, row and head strides ldk, hsk / ldv, hsv in
+ *             elements, multiples of 16 bytes
+ *   dCu       device, int32 [n_seqs + 1], ascending; rows from cu[n_seqs] on are padding and not looked at
+ *   dCos, dSin  device, float [rows][rot / 2], 16-byte aligned; both NULL (rot 0): keys are not rotated
+ *   rot       a multiple of 16 up to head_dim
+ * A page that the call writes must belong to one sequence (its one table entry), and no other call may use it at the same time.
+ */
+int rvq_cache8_append(const rvq_cache8 *cache, const void *dK, const void *dV, int32_t dtype, int64_t rows,
+                      int64_t ldk, int64_t hsk, int64_t ldv, int64_t hsv, const int32_t *dCu,
+                      const float *dCos, const float *dSin, int32_t rot, int32_t layout, void *stream);
+
+/*
+ * Read back: row cu[b] + i is the token of sequence b at position first[b] + i; value = code * scale, rounded
+ * once to dtype.  With tables, keys are rotated by the negative angle: as they were before the rotation, which
+ * is what rvq_encode takes (Section 3: quantized before the rotary embedding).  Tokens that are not in the cache (position
+ * outside [0, lengths[b]), no page) read as 0.  Rows from cu[n_seqs] on are left as they were.
+ *   dFirst    device, int32 [n_seqs]
+ *   dK, dV    device, dtype [rows][n_kv_heads][head_dim], 16-byte aligned, strides as above; either may be NULL
+ * Other arguments as for rvq_cache8_append.
+ */
+int rvq_cache8_read(const rvq_cache8 *cache, const int32_t *dCu, const int32_t *dFirst, int64_t rows,
+                    const float *dCos, const float *dSin, int32_t rot, int32_t layout, int32_t dtype, void *dK,
+                    int64_t ldk, int64_t hsk, void *dV, int64_t ldv, int64_t hsv, void *stream);
+
+/*
+ * Attention of the step's query tokens over the cache, after rvq_cache8_append of the same step.  Row cu[b] + i is
+ * the query token of sequence b at position p = lengths[b] - n_b + i; its query head a attends with kv head
+ * a / rep, rep = n_q_heads / n_kv_heads, to the tokens
+ *   t <= p                                      if window == 0,
+ *   t <= p and (t > p - window or t < sinks)    if window > 0
+ * (a sliding window, and a few first tokens that stay visible):
+ *   out[a] = sum_t softmax_t(scale * q[a] . k[t, a / rep]) v[t, a / rep]
+ * A row that sees nothing is 0.  What hidden and unwritten slots hold, NaN included, does not reach the result.
+ * Scores, maxima, sums and weighted values are fp32; codes enter the matrix cores exactly, queries and weights as
+ * fp16 (fp32 queries: two fp16 terms of each), see the kernel for the roundings.
+ *   dQ      device, dtype [rows][n_q_heads][head_dim], 16-byte aligned, strides ldq, hsq in elements, multiples of
+ *           16 bytes: already rotated
+ *   dOut    the same with ldo, hso; dtype as dQ.  Must not overlap dQ.  Rows from cu[n_seqs] on are left as they were
+ *   n_q_heads   a multiple of n_kv_heads
+ *   dWorkspace  device, 16-byte aligned, workspace_bytes >= rvq_cache8_attn_workspace_bytes() of the same sizes on the
+ *               current device; caller-owned, contents unspecified before and after
+ * A table may name a page several times and share pages between sequences.
+ * rvq_cache8_attn_workspace_bytes returns 0 for sizes that rvq_cache8_attn refuses.
+ */
+int64_t rvq_cache8_attn_workspace_bytes(const rvq_cache8 *cache, int32_t dtype, int64_t rows, int32_t n_q_heads);
+int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int64_t rows, int32_t n_q_heads,
+                    int64_t ldq, int64_t hsq, const int32_t *dCu, float scale, int32_t window, int32_t sinks,
+                    void *dOut, int64_t ldo, int64_t hso, void *dWorkspace, int64_t workspace_bytes, void *stream);
+
 
 /*
  * Packed code storage (Section 3.2: the compression rate of 5.5x counts log2(K) bits per code and a

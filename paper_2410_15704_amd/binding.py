@@ -31,13 +31,23 @@ EXPORTS = ("rvq_create", "rvq_destroy", "rvq_set_codebooks", "rvq_get_codebooks"
            "rvq_get_counters", "rvq_packed_record_bytes", "rvq_pack_codes", "rvq_unpack_codes",
            "rvq_decode_packed", "rvq_decode_rope", "rvq_reserve", "rvq_reserved_rows",
            "rvq_check_kernels", "rvq_debug_set_wait_polls", "rvq_encode_static",
-           "rvq_probe_gather_rates", "rvq_attn_decode", "rvq_attn_workspace_bytes")
+           "rvq_probe_gather_rates", "rvq_attn_decode", "rvq_attn_workspace_bytes",
+           "rvq_rope_tables", "rvq_rope", "rvq_cache8_append", "rvq_cache8_read",
+           "rvq_cache8_attn", "rvq_cache8_attn_workspace_bytes")
+ROPE_ADJACENT, ROPE_HALVES = 0, 1
+PAGE_TOKENS = 64
 
 
 class rvq_config(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "d", "dhat", "depth", "K", "grouping", "scale", "std_ddof", "in_dtype", "out_dtype",
         "std_dtype", "encode_path", "reserved")]
+
+
+class rvq_cache8(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("table_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("lengths", ctypes.c_void_p)]
 
 
 def _load():
@@ -75,10 +85,18 @@ def _load():
     lib.rvq_attn_workspace_bytes.argtypes = [i64, i32, i32]
     lib.rvq_attn_workspace_bytes.restype = i64
     lib.rvq_attn_decode.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp, i32, i64, vp, vp, f32, vp, vp, i64, vp]
+    f64, view = ctypes.c_double, ctypes.POINTER(rvq_cache8)
+    lib.rvq_rope_tables.argtypes = [vp, i64, i32, f64, f64, f64, f64, f64, f64, vp, vp, vp]
+    lib.rvq_rope.argtypes = [vp, i32, i64, i32, i32, i32, i32, i64, i64, vp, vp, vp, i64, i64, vp]
+    lib.rvq_cache8_append.argtypes = [view, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, vp, i32, i32, vp]
+    lib.rvq_cache8_read.argtypes = [view, vp, vp, i64, vp, vp, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp]
+    lib.rvq_cache8_attn_workspace_bytes.argtypes = [view, i32, i64, i32]
+    lib.rvq_cache8_attn_workspace_bytes.restype = i64
+    lib.rvq_cache8_attn.argtypes = [view, vp, i32, i64, i32, i64, i64, vp, f32, i32, i32, vp, i64, i64, vp, i64, vp]
     for name in EXPORTS:
         getattr(lib, name)
         if name not in ("rvq_strerror", "rvq_version", "rvq_packed_record_bytes",
-                        "rvq_reserved_rows", "rvq_attn_workspace_bytes"):
+                        "rvq_reserved_rows", "rvq_attn_workspace_bytes", "rvq_cache8_attn_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_int
     return lib
 
@@ -343,3 +361,186 @@ class Quantizer:
                    code_stride=1):
         rvq_ema_update(self.ctx, stage, R, codes, code_stride, R.shape[0], decay, eps,
                        cluster_size, embed_sum)
+
+
+# ---- rotary positions and the paged cache of 8-bit codes: tensors in, tensors out ---------------
+# Checks of types, shapes and devices; sizes, strides and alignment are checked by the entry points.  The work goes to the
+# current stream of the tensors' device.
+_ELEMENTS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _dtype(t, what):
+    code = _ELEMENTS.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what}: fp32, bf16 or fp16 expected, got {t.dtype}")
+    return code
+
+
+def _whole(t, what, dtype, shape, device):
+    """A contiguous tensor of that type and shape on that device."""
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {dtype} {tuple(shape)} on {device} expected, got {t.dtype} "
+                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _heads(t, what, heads, hd, device, rows=None):
+    """[rows][heads][hd] with neighbouring channels."""
+    if t.dim() != 3 or t.device != device or t.shape[1] != heads or t.shape[2] != hd or t.stride(2) != 1 or (
+            rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{what}: [{'rows' if rows is None else rows}][{heads}][{hd}] with neighbouring channels on "
+                         f"{device} expected, got {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+class _On:
+    """The call's device current in this thread, as the entry points want it; nothing to do where it is already."""
+
+    def __init__(self, device):
+        if device.type != "cuda":
+            raise ValueError(f"tensors on a GPU expected, got {device}")
+        self.want = device.index if device.index is not None else torch.cuda.current_device()
+
+    def __enter__(self):
+        self.was = torch.cuda.current_device()
+        if self.was != self.want:
+            torch.cuda.set_device(self.want)
+
+    def __exit__(self, *exc):
+        if self.was != self.want:
+            torch.cuda.set_device(self.was)
+
+
+def _tables(cos, sin, rows, device):
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin belong together")
+    if cos is None:
+        return None, None, 0
+    half = cos.shape[-1]
+    return (_whole(cos, "cos", torch.float32, (rows, half), device), _whole(sin, "sin", torch.float32, (rows, half), device),
+            2 * half)
+
+
+def rope_tables(positions, rot, base=10000.0, factor=1.0, orig_len=0.0, alpha=1.0, beta=32.0, amplitude=1.0, out=None):
+    """cos, sin, fp32 [N][rot / 2], of int64 positions [N] (rvq_rope_tables); out: a pair of such tensors."""
+    N, dev = positions.numel(), positions.device
+    p = _whole(positions, "positions", torch.int64, (N,), dev)
+    with _On(dev):
+        if out is None:
+            both = torch.empty((2, N, max(rot, 0) // 2), dtype=torch.float32, device=dev)
+            out = both[0], both[1]
+        cos, sin = out
+        c, s = (_whole(t, "out", torch.float32, (N, max(rot, 0) // 2), dev) for t in out)
+        _chk(lib.rvq_rope_tables(p, N, rot, base, factor, orig_len, alpha, beta, amplitude, c, s, _stream(None)), None)
+    return cos, sin
+
+
+def rope(x, cos, sin, layout=ROPE_ADJACENT, out=None):
+    """Head vectors x [N][heads][head_dim] with the first 2 * cos.shape[1] channels of each rotated (rvq_rope).
+    out: a tensor like x, x itself to rotate in place; rows and heads may be strided in both."""
+    dtype, dev = _dtype(x, "x"), x.device
+    if x.dim() != 3:
+        raise ValueError(f"x: [rows][heads][head_dim] expected, got {tuple(x.shape)}")
+    N, heads, hd = x.shape
+    px, ldx, hsx = _heads(x, "x", heads, hd, dev)
+    c, s, rot = _tables(cos, sin, N, dev)
+    with _On(dev):
+        if out is None:
+            out = torch.empty((N, heads, hd), dtype=x.dtype, device=dev)
+        if out.dtype != x.dtype:
+            raise ValueError(f"out: {x.dtype} expected, got {out.dtype}")
+        po, ldo, hso = _heads(out, "out", heads, hd, dev, N)
+        _chk(lib.rvq_rope(px, dtype, N, heads, hd, rot, layout, ldx, hsx, c, s, po, ldo, hso, _stream(None)), None)
+    return out
+
+
+class Cache8:
+    """Paged cache of keys and values in 8 bits (rvq_cache8): owns, or is given, the codes `pages`, uint8
+    [n_pages][n_kv_heads][2][64 * head_dim], and `scales`, fp32 [n_pages][n_kv_heads][2].
+
+    A step brings rows cu[b] .. cu[b + 1] of sequence b; `lengths` counts every sequence's tokens with them, `table`
+    [sequences][entries] names its pages.  All three are int32 tensors on the device, so that a captured step can be
+    replayed with other lengths and pages.  Which pages are free is the caller's business."""
+
+    def __init__(self, pages, scales):
+        if pages.dim() != 4 or pages.shape[2] != 2 or pages.shape[3] % PAGE_TOKENS:
+            raise ValueError(f"pages: [n_pages][n_kv_heads][2][{PAGE_TOKENS} * head_dim] expected, got {tuple(pages.shape)}")
+        self.device = pages.device
+        self.n_pages, self.n_kv_heads, self.head_dim = pages.shape[0], pages.shape[1], pages.shape[3] // PAGE_TOKENS
+        p = _whole(pages, "pages", torch.uint8, pages.shape, self.device)
+        s = _whole(scales, "scales", torch.float32, pages.shape[:3], self.device)
+        self.pages, self.scales = pages, scales
+        self._pool = p, s, self.n_pages, self.n_kv_heads, self.head_dim
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, head_dim, device="cuda"):
+        shape = (n_pages, n_kv_heads, 2, PAGE_TOKENS * head_dim)
+        return cls(torch.zeros(shape, dtype=torch.uint8, device=device), torch.zeros(shape[:3], dtype=torch.float32, device=device))
+
+    def _step(self, cu, table, lengths):
+        n = lengths.shape[0] if lengths.dim() == 1 else -1
+        if table.dim() != 2:
+            raise ValueError(f"table: [sequences][entries] expected, got {tuple(table.shape)}")
+        view = rvq_cache8(*self._pool, _whole(table, "table", torch.int32, (n, table.shape[1]), self.device), table.shape[1], n,
+                          _whole(lengths, "lengths", torch.int32, (n,), self.device))
+        return ctypes.byref(view), _whole(cu, "cu", torch.int32, (n + 1,), self.device)
+
+    def append(self, k, v, cu, table, lengths, cos=None, sin=None, layout=ROPE_ADJACENT):
+        """Stores the step's keys, rotated when tables are given, and values, [rows][n_kv_heads][head_dim] (rvq_cache8_append)."""
+        view, pcu = self._step(cu, table, lengths)
+        dtype, rows = _dtype(k, "k"), k.shape[0]
+        if v.dtype != k.dtype:
+            raise ValueError(f"v: {k.dtype} expected, got {v.dtype}")
+        pk, ldk, hsk = _heads(k, "k", self.n_kv_heads, self.head_dim, self.device)
+        pv, ldv, hsv = _heads(v, "v", self.n_kv_heads, self.head_dim, self.device, rows)
+        c, s, rot = _tables(cos, sin, rows, self.device)
+        with _On(self.device):
+            _chk(lib.rvq_cache8_append(view, pk, pv, dtype, rows, ldk, hsk, ldv, hsv, pcu, c, s, rot, layout, _stream(None)), None)
+
+    def read(self, rows, cu, first, table, lengths, dtype=torch.float16, cos=None, sin=None, layout=ROPE_ADJACENT, out=None):
+        """k, v [rows][n_kv_heads][head_dim]: row cu[b] + i is the token of sequence b at position first[b] + i; with
+        tables, keys as they were before the rotation (rvq_cache8_read).  out: a pair of such tensors."""
+        view, pcu = self._step(cu, table, lengths)
+        pf = _whole(first, "first", torch.int32, lengths.shape, self.device)
+        c, s, rot = _tables(cos, sin, rows, self.device)
+        with _On(self.device):
+            if out is None:
+                both = torch.empty((2, rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
+                out = both[0], both[1]
+            k, v = out
+            code = _dtype(k, "out")
+            if v.dtype != k.dtype:
+                raise ValueError(f"out: one type expected, got {k.dtype} and {v.dtype}")
+            pk, ldk, hsk = _heads(k, "out", self.n_kv_heads, self.head_dim, self.device, rows)
+            pv, ldv, hsv = _heads(v, "out", self.n_kv_heads, self.head_dim, self.device, rows)
+            _chk(lib.rvq_cache8_read(view, pcu, pf, rows, c, s, rot, layout, code, pk, ldk, hsk, pv, ldv, hsv, _stream(None)), None)
+        return k, v
+
+    def workspace_bytes(self, q):
+        """Bytes of workspace that attend() needs for queries of that shape and type."""
+        with _On(self.device):
+            view = rvq_cache8(*self._pool, None, 1, 1, None)  # the size does not depend on the sequences
+            return lib.rvq_cache8_attn_workspace_bytes(ctypes.byref(view), _dtype(q, "q"), q.shape[0], q.shape[1])
+
+    def attend(self, q, cu, table, lengths, scale=None, window=0, sinks=0, out=None, workspace=None):
+        """Attention of the step's query tokens q [rows][heads][head_dim], already rotated, over the cache
+        (rvq_cache8_attn).  scale: 1 / sqrt(head_dim) if not given; workspace: uint8 of workspace_bytes(q), allocated if not given."""
+        view, pcu = self._step(cu, table, lengths)
+        dtype = _dtype(q, "q")
+        if q.dim() != 3:
+            raise ValueError(f"q: [rows][heads][head_dim] expected, got {tuple(q.shape)}")
+        rows, heads, hd = q.shape
+        pq, ldq, hsq = _heads(q, "q", heads, self.head_dim, self.device)
+        with _On(self.device):
+            if out is None:
+                out = torch.empty((rows, heads, hd), dtype=q.dtype, device=self.device)
+            if out.dtype != q.dtype:
+                raise ValueError(f"out: {q.dtype} expected, got {out.dtype}")
+            po, ldo, hso = _heads(out, "out", heads, hd, self.device, rows)
+            if workspace is None:
+                need = lib.rvq_cache8_attn_workspace_bytes(view, dtype, rows, heads)
+                workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+            pw = _whole(workspace, "workspace", torch.uint8, workspace.shape, self.device)
+            _chk(lib.rvq_cache8_attn(view, pq, dtype, rows, heads, ldq, hsq, pcu, scale if scale is not None else hd**-0.5, window,
+                                     sinks, po, ldo, hso, pw, workspace.numel(), _stream(None)), None)
+        return out

@@ -92,7 +92,7 @@ int encode_enqueue(rvq_ctx *ctx, const void *dX, int64_t N, int64_t ldx, int sta
 
 extern "C" {
 
-int rvq_version(void) { return 1000; }
+int rvq_version(void) { return 1001; }
 
 const char *rvq_strerror(int code) {
   switch (code) {

@@ -1,0 +1,502 @@
+// Attention over the paged cache of 8-bit codes, for the query tokens of a step.
+//
+// Work.  The query heads that share a kv head, times the query tokens of a sequence, are columns; an item is a
+// block of columns of one (sequence, kv head), a unit one page of an item.  Units are numbered sequence by
+// sequence, and every workgroup takes an equal run of them, whatever the lengths: it walks the run
+// item by item, and where it holds all pages of an item it writes the rows, else a partial result (maximum, sum,
+// weighted values of every column), which a second kernel joins.  The numbering needs the lengths, which only
+// the device knows, so every workgroup computes it: a prefix sum over the sequences.
+//
+// Arithmetic of a page (64 tokens) and 16 columns, all in one wavefront and without any exchange but two lane
+// moves for the maximum:
+//   scores^T = K q^T    16x16x32 products, rows = tokens, columns = query heads
+//   weights             2^(s - m) of the same registers
+//   out^T += V^T w^T    rows = channels, contraction over tokens
+// A lane of the first product's result holds 4 tokens of its column per tile; the tokens are dealt to the tiles' rows
+// so that the four tiles give a lane of group g (lane / 16) the tokens 16 g .. 16 g + 15, which is what it feeds the
+// second product.  The cache's layout is made for it: a lane reads 16 bytes of a key (channels 16 g ..) or of a
+// value channel (tokens 16 g ..) and converts them in pairs to fp16, which holds every e4m3 number exactly.
+//
+// Roundings.  Queries: scaled by a power of two to a largest element in [2^8, 2^9) and rounded to fp16 (exact for bf16 and
+// fp16 but for elements below 2^-22 of the largest); fp32 queries are split into two fp16 terms, 22 bits.  Weights: 2^14 2^(s - m), so
+// that fp16 holds them with 11 bits down to 2^-28 of the largest; with fp32 queries two terms of them as
+// well.  Sums in fp32 (weights before their rounding), products accumulate in fp32.
+//
+// The scale of a page's keys enters the scores' factor.  Its values' scale becomes the unit of the accumulators,
+// which are multiplied by the powers of two between units along with the correction of the maximum.
+#include <cmath>
+
+#include "rvq_cache8.h"
+
+namespace {
+
+constexpr float NEG = -3.402823466e38f;  // "nothing yet": finite, so that differences are numbers
+constexpr float WEIGHT_BITS = 14.0f;     // weights are held as 2^14 2^(s - m)
+constexpr int COLS = 16;                 // columns of an item
+constexpr int WAVES = 4;
+
+struct AttnArgs {
+  CacheView c;
+  const void *q;
+  void *out;
+  int64_t ldq, hsq, ldo, hso;
+  int rep, window, sinks;
+  float scale;  // log2(e) times the softmax scale
+  float *part;      // [2 * workgroups][COLS][HD + 2]
+  int64_t *header;  // [workgroups][8]
+  int64_t least;    // fewest units of a workgroup
+};
+
+// what a sequence's queries see: pages [0, sink_pages) and [begin, end) of its table
+struct Seen {
+  SeqRows r;
+  int64_t p0;     // position of the first query token
+  int64_t tokens; // tokens that have an entry in the table
+  int64_t sink_pages, begin, pages;
+  int blocks;     // of columns
+};
+__device__ __forceinline__ Seen seen_by(const AttnArgs &a, int b) {
+  Seen s;
+  s.r = rows_of(a.c, b);
+  const int64_t len = a.c.lengths[b] < 0 ? 0 : a.c.lengths[b], room = (int64_t)a.c.table_pages * PAGE;
+  s.p0 = len - s.r.n;
+  s.tokens = len < room ? len : room;
+  int64_t begin = a.window > 0 ? s.p0 - a.window + 1 : 0;
+  s.begin = (begin < 0 ? 0 : begin) / PAGE;
+  const int64_t end = (s.tokens + PAGE - 1) / PAGE;
+  int64_t sink = a.window > 0 ? ((int64_t)a.sinks + PAGE - 1) / PAGE : 0;
+  sink = sink < s.begin ? sink : s.begin;
+  s.sink_pages = sink < end ? sink : end;
+  const int64_t windowed = end > s.begin ? end - s.begin : 0;
+  s.pages = s.sink_pages + windowed;
+  if (s.pages < 1) s.pages = 1;  // rows that see nothing are written too
+  s.blocks = (int)(((int64_t)s.r.n * a.rep + COLS - 1) / COLS);
+  return s;
+}
+__device__ __forceinline__ int64_t units_of(const AttnArgs &a, int b) {
+  const Seen s = seen_by(a, b);
+  return (int64_t)s.blocks * a.c.heads * s.pages;
+}
+
+// units of a workgroup's run, computed by every wavefront
+__device__ __forceinline__ int64_t run_length(const AttnArgs &a) {
+  const int lane = threadIdx.x & 63;
+  int64_t total = 0;
+  for (int b = lane; b < a.c.n_seqs; b += 64) total += units_of(a, b);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d, 64);
+  const int64_t even = (total + gridDim.x - 1) / gridDim.x;
+  return even > a.least ? even : a.least;
+}
+
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x) |
+                   ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32));
+}
+
+// 8 codes -> 8 fp16 numbers, exactly
+__device__ __forceinline__ f16x8 widen8(uint32_t lo, uint32_t hi) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+  f16x8 r;
+  r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1];
+  r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
+  return r;
+}
+// bytes that are NaN codes, as 0x80 in their place
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+// nearest of eight floats as fp16, or what that leaves
+__device__ __forceinline__ f16x8 half8(const float (&x)[8]) {
+  f16x8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (_Float16)x[i];
+  return r;
+}
+__device__ __forceinline__ f16x8 rest8(const float (&x)[8], f16x8 hi) {
+  f16x8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (_Float16)(x[i] - (float)hi[i]);
+  return r;
+}
+
+template <typename T, int HD> struct Columns {
+  static constexpr bool SPLIT = std::is_same<T, float>::value;
+  static constexpr int PARTS = HD / 32;  // products of 32 channels
+  f16x8 hi[PARTS], lo[SPLIT ? PARTS : 1];
+  float factor;  // of a score, but for the keys' scale
+  int64_t p;     // position of this lane's column; -1: no such column
+};
+
+template <typename T, int HD>
+__device__ __forceinline__ void load_columns(const AttnArgs &a, const Seen &s, int head, int block, Columns<T, HD> &k) {
+  typedef Columns<T, HD> C;
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  const int64_t c = (int64_t)block * COLS + (lane & 15), token = c / a.rep;
+  const bool valid = token < s.r.n;
+  float x[C::PARTS][8];
+  float amax = 0.0f;
+  if (valid) {
+    const T *q = (const T *)a.q + (s.r.row + token) * a.ldq + ((int64_t)head * a.rep + (c - token * a.rep)) * a.hsq;
+#pragma unroll
+    for (int m = 0; m < C::PARTS; ++m) load8<T>(q + (m >> 1) * 64 + g * 16 + (m & 1) * 8, x[m]);
+  } else {
+#pragma unroll
+    for (int m = 0; m < C::PARTS; ++m)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[m][i] = 0.0f;
+  }
+#pragma unroll
+  for (int m = 0; m < C::PARTS; ++m)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(x[m][i]));
+  amax = fmaxf(amax, __shfl_xor(amax, 16, 64));
+  amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
+  int e = (int)(__float_as_uint(amax) >> 23) - 127 - 8;  // largest element to [2^8, 2^9)
+  e = e < -118 ? -118 : e;
+  const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+  k.factor = ldexpf(a.scale, e);
+  k.p = valid ? s.p0 + token : -1;
+#pragma unroll
+  for (int m = 0; m < C::PARTS; ++m) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[m][i] *= down;
+    k.hi[m] = half8(x[m]);
+    if constexpr (C::SPLIT) k.lo[m] = rest8(x[m], k.hi[m]);
+  }
+}
+
+// one wavefront's running result of 16 columns: lane (column n, group g) holds channels 16 t + 4 g + r
+template <int HD> struct State {
+  f32x4 acc[HD / 16];
+  float m, l, unit;  // maximum (base 2), sum of this lane's weights, scale of the accumulators
+};
+
+template <typename T, int HD>
+__device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD> &k, State<HD> &st, int64_t page, int head,
+                                          int64_t t0, int64_t tokens, bool whole) {
+  typedef Columns<T, HD> C;
+  const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+  const uint8_t *kc = codes_of(a.c, page, head, 0), *vc = codes_of(a.c, page, head, 1);
+  const f32x2 scales = *reinterpret_cast<const f32x2 *>(scale_of(a.c, page, head, 0));
+  u32x4 kw[4][HD / 64], vw[HD / 16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < HD / 64; ++j)  // row n of tile i is token 16 (n / 4) + 4 i + n % 4
+      kw[i][j] = *reinterpret_cast<const u32x4 *>(kc + ((n >> 2) * 16 + i * 4 + (n & 3)) * HD + j * 64 + g * 16);
+#pragma unroll
+  for (int t = 0; t < HD / 16; ++t) vw[t] = *reinterpret_cast<const u32x4 *>(vc + (t * 16 + n) * PAGE + g * 16);
+
+  const float factor = k.factor * scales[0];
+  float s[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f32x4 d = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < HD / 64; ++j) {
+      const f16x8 x = widen8(kw[i][j][0], kw[i][j][1]), y = widen8(kw[i][j][2], kw[i][j][3]);
+      if constexpr (C::SPLIT) {
+        d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, k.lo[2 * j], d, 0, 0, 0);
+        d = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, k.lo[2 * j + 1], d, 0, 0, 0);
+      }
+      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, k.hi[2 * j], d, 0, 0, 0);
+      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, k.hi[2 * j + 1], d, 0, 0, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[4 * i + r] = d[r] * factor;
+  }
+  bool visible[16];
+  if (!whole) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int64_t t = t0 + g * 16 + i;
+      visible[i] = t <= k.p && t < tokens && (a.window <= 0 || t > k.p - a.window || t < a.sinks);
+      s[i] = visible[i] ? s[i] : -INFINITY;
+    }
+  }
+  float top = st.m;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  float fix = __builtin_amdgcn_exp2f(st.m - top);
+  st.m = top;
+  st.l *= fix;
+  // the accumulators' unit becomes this page's scale; a step of more than 2^40 downwards is left to the weights
+  float unit = scales[1], rest = 1.0f;
+  if (unit < st.unit * 0x1p-40f) {
+    unit = st.unit * 0x1p-40f;
+    rest = scales[1] / unit;
+  }
+  fix *= st.unit / unit;
+  st.unit = unit;
+  float w[2][8];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float x = __builtin_amdgcn_exp2f(s[i] - (top - WEIGHT_BITS));
+    st.l += x;
+    w[i >> 3][i & 7] = x * rest;
+  }
+  f16x8 hi[2], lo[C::SPLIT ? 2 : 1];
+  hi[0] = half8(w[0]);
+  hi[1] = half8(w[1]);
+  if constexpr (C::SPLIT) {
+    lo[0] = rest8(w[0], hi[0]);
+    lo[1] = rest8(w[1], hi[1]);
+  }
+  // A NaN in a slot that a column does not see must not meet its weight of 0: take such codes out, and count, for
+  // each (channel, column), the NaN that it does see.
+  uint32_t bad = 0;
+  if (!whole) {
+#pragma unroll
+    for (int t = 0; t < HD / 16; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bad |= nan_bytes(vw[t][i]);
+    bad = __ballot(bad != 0) != 0;
+  }
+  if (bad) {
+    f16x8 sees[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sees[i >> 3][i & 7] = visible[i] ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+    for (int t = 0; t < HD / 16; ++t) {
+      u32x4 mark;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t b = nan_bytes(vw[t][i]) >> 7;  // 1 in the place of a NaN
+        mark[i] = b * 0x38u;                          // the code of 1.0
+        vw[t][i] &= ~(b * 0xffu);
+      }
+      f32x4 d = {0, 0, 0, 0};
+      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(mark[0], mark[1]), sees[0], d, 0, 0, 0);
+      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(mark[2], mark[3]), sees[1], d, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (d[r] > 0.0f) st.acc[t][r] = __uint_as_float(0x7fc00000u);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < HD / 16; ++t) {
+    const f16x8 x = widen8(vw[t][0], vw[t][1]), y = widen8(vw[t][2], vw[t][3]);
+    f32x4 d = st.acc[t] * fix;
+    if constexpr (C::SPLIT) {
+      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, lo[0], d, 0, 0, 0);
+      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, lo[1], d, 0, 0, 0);
+    }
+    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, hi[0], d, 0, 0, 0);
+    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, hi[1], d, 0, 0, 0);
+    st.acc[t] = d;
+  }
+}
+
+// header of a workgroup whose last item goes on in the next runs: what the joining kernel needs
+enum { H_PARTS = 0, H_FIRST, H_ROW, H_COLS, H_HEAD, H_COL0 };
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_kernel(const AttnArgs a) {
+  __shared__ float sh_acc[WAVES][COLS][HD + 4];
+  __shared__ float sh_m[WAVES][COLS], sh_l[WAVES][COLS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, n = lane & 15;
+  const int64_t run = run_length(a), w = blockIdx.x;
+  const int64_t u0 = w * run;
+  int b;
+  int64_t inside;
+  if (threadIdx.x == 0) a.header[w * 8 + H_PARTS] = 0;
+  if (!find_piece(a.c.n_seqs, u0, [&](int i) { return units_of(a, i); }, b, inside)) return;
+  b = __builtin_amdgcn_readfirstlane(b);
+  inside = uniform(inside);
+  int64_t left = run;
+  bool at_start = true;
+  while (left > 0 && b < a.c.n_seqs) {
+    const Seen s = seen_by(a, b);
+    const int64_t items = (int64_t)s.blocks * a.c.heads;
+    int64_t item = inside / s.pages, x = inside - item * s.pages;
+    for (; item < items && left > 0; ++item, x = 0) {
+      const int head = (int)(item / s.blocks), block = (int)(item - (int64_t)head * s.blocks);
+      const int64_t end = x + left < s.pages ? x + left : s.pages;
+      left -= end - x;
+      Columns<T, HD> k;
+      load_columns<T, HD>(a, s, head, block, k);
+      const int64_t col0 = (int64_t)block * COLS, most = (int64_t)s.r.n * a.rep - col0;
+      const int cols = most < COLS ? (int)most : COLS;
+      const int64_t first = s.p0 + col0 / a.rep, last = s.p0 + (col0 + cols - 1) / a.rep;
+      State<HD> st;
+#pragma unroll
+      for (int t = 0; t < HD / 16; ++t) st.acc[t] = f32x4{0, 0, 0, 0};
+      st.m = NEG;
+      st.l = 0.0f;
+      st.unit = 1.0f;
+      for (int64_t i = x + wave; i < end; i += WAVES) {
+        const int64_t entry = i < s.sink_pages ? i : s.begin + i - s.sink_pages, t0 = entry * PAGE;
+        if (t0 > last || t0 >= s.tokens) continue;
+        if (a.window > 0 && t0 + PAGE <= first - a.window + 1 && t0 >= a.sinks) continue;
+        const int64_t page = page_of(a.c, b, entry);
+        if (page < 0) continue;
+        const bool whole = t0 + PAGE - 1 <= first && t0 + PAGE <= s.tokens &&
+                           (a.window <= 0 || t0 > last - a.window || t0 + PAGE <= a.sinks);
+        take_page<T, HD>(a, k, st, uniform(page), head, t0, s.tokens, whole);
+      }
+      // the wavefronts' results together
+      st.l += __shfl_xor(st.l, 16, 64);
+      st.l += __shfl_xor(st.l, 32, 64);
+      if (g == 0) {
+        sh_m[wave][n] = st.m;
+        sh_l[wave][n] = st.l;
+      }
+#pragma unroll
+      for (int t = 0; t < HD / 16; ++t)
+        *reinterpret_cast<f32x4 *>(&sh_acc[wave][n][t * 16 + g * 4]) = st.acc[t] * st.unit;
+      __syncthreads();
+      const int c = threadIdx.x >> 4, ch0 = (threadIdx.x & 15) * (HD / 16);
+      float top = NEG, sum = 0.0f, weight[WAVES];
+#pragma unroll
+      for (int v = 0; v < WAVES; ++v) top = fmaxf(top, sh_m[v][c]);
+#pragma unroll
+      for (int v = 0; v < WAVES; ++v) {
+        weight[v] = __builtin_amdgcn_exp2f(sh_m[v][c] - top);
+        sum += weight[v] * sh_l[v][c];
+      }
+      float o[HD / 16];
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) {
+        o[i] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) o[i] += weight[v] * sh_acc[v][c][ch0 + i];
+      }
+      const bool all = x == 0 && end == s.pages;
+      if (c < cols) {
+        if (all) {
+          const int64_t token = (col0 + c) / a.rep, h = (int64_t)head * a.rep + (col0 + c - token * a.rep);
+          T *out = (T *)a.out + (s.r.row + token) * a.ldo + h * a.hso + ch0;
+          const float over = sum != 0.0f ? 1.0f / sum : 0.0f;  // nothing seen: 0
+#pragma unroll
+          for (int i = 0; i < HD / 16; ++i) out[i] = (T)(sum != 0.0f ? o[i] * over : 0.0f);
+        } else {
+          float *p = a.part + ((2 * w + (at_start ? 0 : 1)) * COLS + c) * (HD + 2);
+#pragma unroll
+          for (int i = 0; i < HD / 16; ++i) p[ch0 + i] = o[i];
+          if ((threadIdx.x & 15) == 0) {
+            p[HD] = top;
+            p[HD + 1] = sum;
+          }
+        }
+      }
+      if (x == 0 && end < s.pages && threadIdx.x == 0) {
+        int64_t *hd = a.header + w * 8;
+        hd[H_PARTS] = 1 + (s.pages - end + run - 1) / run;
+        hd[H_FIRST] = 2 * w + (at_start ? 0 : 1);
+        hd[H_ROW] = s.r.row;
+        hd[H_COLS] = cols;
+        hd[H_HEAD] = head;
+        hd[H_COL0] = col0;
+      }
+      at_start = false;
+      __syncthreads();
+    }
+    ++b;
+    inside = 0;
+  }
+}
+
+// Joins the parts of the item that begins in run blockIdx.x and goes on: a wavefront per column.  The first part lies at
+// H_FIRST, the others at the beginnings of the following runs.
+template <typename T, int HD> __global__ __launch_bounds__(256) void cache8_join_kernel(const AttnArgs a) {
+  const int64_t w = blockIdx.x;
+  const int64_t *hd = a.header + w * 8;
+  const int64_t parts = hd[H_PARTS];
+  const int c = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (!parts || c >= hd[H_COLS]) return;
+  const auto part = [&](int64_t i) { return a.part + ((i ? 2 * (w + i) : hd[H_FIRST]) * COLS + c) * (HD + 2); };
+  float top = NEG;
+  for (int64_t i = lane; i < parts; i += 64) top = fmaxf(top, part(i)[HD]);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+  float sum = 0.0f, o[HD / 64];
+#pragma unroll
+  for (int j = 0; j < HD / 64; ++j) o[j] = 0.0f;
+#pragma unroll 8
+  for (int64_t i = 0; i < parts; ++i) {
+    const float *p = part(i);
+    const float x = __builtin_amdgcn_exp2f(p[HD] - top);
+    sum += x * p[HD + 1];
+#pragma unroll
+    for (int j = 0; j < HD / 64; ++j) o[j] += x * p[j * 64 + lane];
+  }
+  const int64_t col = hd[H_COL0] + c, token = col / a.rep, h = hd[H_HEAD] * a.rep + (col - token * a.rep);
+  T *out = (T *)a.out + (hd[H_ROW] + token) * a.ldo + h * a.hso;
+  const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+  for (int j = 0; j < HD / 64; ++j) out[j * 64 + lane] = (T)(sum != 0.0f ? o[j] * over : 0.0f);
+}
+
+template <typename T, int HD> void launch_attn(const AttnArgs &a, int groups, hipStream_t s) {
+  hipLaunchKernelGGL((cache8_attn_kernel<T, HD>), dim3(groups), dim3(64 * WAVES), 0, s, a);
+  const int64_t cols = a.c.rows * a.rep < COLS ? a.c.rows * a.rep : COLS;
+  hipLaunchKernelGGL((cache8_join_kernel<T, HD>), dim3(groups, (unsigned)(cols + 3) / 4), dim3(256), 0, s, a);
+}
+template <typename T> void launch_attn_hd(const AttnArgs &a, int groups, hipStream_t s) {
+  if (a.c.hd == 64) launch_attn<T, 64>(a, groups, s);
+  else if (a.c.hd == 128) launch_attn<T, 128>(a, groups, s);
+  else launch_attn<T, 256>(a, groups, s);
+}
+
+// workgroups: two on every CU
+int attn_groups() {
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1) {
+    (void)hipGetLastError();
+    return 0;
+  }
+  return 2 * cus;
+}
+
+bool attn_ok(const rvq_cache8 *c, int32_t dtype, int64_t rows, int32_t n_q_heads) {
+  if (!rvq_cache8_ok(c) || rows < 0 || rows > INT32_MAX) return false;
+  if (dtype != RVQ_F32 && dtype != RVQ_BF16 && dtype != RVQ_F16) return false;
+  if (n_q_heads < c->n_kv_heads || n_q_heads > 65535 || n_q_heads % c->n_kv_heads) return false;
+  return rows * (n_q_heads / c->n_kv_heads) <= INT32_MAX / 2;  // columns of a sequence
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t rvq_cache8_attn_workspace_bytes(const rvq_cache8 *cache, int32_t dtype, int64_t rows, int32_t n_q_heads) {
+  if (!attn_ok(cache, dtype, rows, n_q_heads)) return 0;
+  const int64_t groups = attn_groups();
+  return groups * 64 + 2 * groups * COLS * (cache->head_dim + 2) * (int64_t)sizeof(float);
+}
+
+int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int64_t rows, int32_t n_q_heads,
+                    int64_t ldq, int64_t hsq, const int32_t *dCu, float scale, int32_t window, int32_t sinks,
+                    void *dOut, int64_t ldo, int64_t hso, void *dWorkspace, int64_t workspace_bytes, void *stream) {
+  if (!attn_ok(cache, dtype, rows, n_q_heads) || !std::isfinite(scale) || window < 0 || sinks < 0) return RVQ_EINVAL;
+  if (rows == 0) return RVQ_OK;
+  const int hd = cache->head_dim;
+  if (!rvq_cache8_pointers_ok(cache) || !rvq_aligned(dCu, 4)) return RVQ_EINVAL;
+  if (!rvq_rows16_ok(dQ, dtype, rows, n_q_heads, hd, ldq, hsq) || !rvq_rows16_ok(dOut, dtype, rows, n_q_heads, hd, ldo, hso) ||
+      !rvq_rows_distinct(rows, n_q_heads, hd, ldo, hso) || dQ == dOut)
+    return RVQ_EINVAL;
+  if (!rvq_aligned(dWorkspace, 16)) return RVQ_EINVAL;
+  const int groups = attn_groups();
+  if (!groups) return RVQ_EHIP;
+  if (workspace_bytes < rvq_cache8_attn_workspace_bytes(cache, dtype, rows, n_q_heads)) return RVQ_EWORKSPACE;
+  if (!rvq_stream_is_current((hipStream_t)stream)) return RVQ_EINVAL;
+  AttnArgs a;
+  a.c = view_of(cache, dCu, rows);
+  a.q = dQ; a.out = dOut;
+  a.ldq = ldq; a.hsq = hsq; a.ldo = ldo; a.hso = hso;
+  a.rep = n_q_heads / cache->n_kv_heads;
+  a.window = window; a.sinks = sinks;
+  a.scale = scale * 1.44269504088896340736f;
+  a.header = (int64_t *)dWorkspace;
+  a.part = (float *)((char *)dWorkspace + (int64_t)groups * 64);
+  a.least = WAVES;
+  if (dtype == RVQ_F32) launch_attn_hd<float>(a, groups, (hipStream_t)stream);
+  else if (dtype == RVQ_BF16) launch_attn_hd<__bf16>(a, groups, (hipStream_t)stream);
+  else launch_attn_hd<_Float16>(a, groups, (hipStream_t)stream);
+  return hipGetLastError() == hipSuccess ? RVQ_OK : RVQ_EHIP;
+}
+
+}  // extern "C"

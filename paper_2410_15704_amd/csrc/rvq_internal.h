@@ -282,3 +282,33 @@ hipError_t rvq_launch_attn_decode(const rvq_ctx *kctx, const rvq_ctx *vctx, cons
                                   const void *dVCodes, const void *dVStd, int packed_bytes, int64_t N,
                                   const float *dCos, const float *dSin, float scale, int k_depth_used,
                                   int v_depth_used, float *dOut, float *dWork, hipStream_t s);
+
+// ---- calls without a context ----
+// whether a stream belongs to the device that is current in this thread (a launch on another one fails)
+inline bool rvq_stream_is_current(hipStream_t s) {
+  if (!s) return true;
+  hipDevice_t of = -1;
+  int current = -2;
+  if (hipStreamGetDevice(s, &of) != hipSuccess || hipGetDevice(&current) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return of == current;
+}
+
+// whether the elements of [N][heads][hd] with these strides are all different ones, so that they can be written
+inline bool rvq_rows_distinct(int64_t N, int64_t heads, int64_t hd, int64_t ld, int64_t hs) {
+  if (N <= 1) return heads <= 1 || hs >= hd;
+  if (heads <= 1) return ld >= hd;
+  if (hs <= ld) return hs >= hd && ld >= hd && (ld - hd) / hs >= heads - 1;
+  return ld >= hd && (hs - hd) / ld >= N - 1;
+}
+
+// whether N rows of these strides stay within 63-bit byte offsets
+inline bool rvq_rows_fit(int64_t N, int64_t heads, int64_t hd, int64_t ld, int64_t hs) {
+  const int64_t most = INT64_MAX / 32;
+  if (ld < 0 || hs < 0) return false;
+  if (N > most / heads / hd) return false;
+  if (ld && N > most / ld) return false;
+  return !hs || heads <= most / hs;
+}
