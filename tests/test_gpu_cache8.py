@@ -367,6 +367,33 @@ def test_attention_over_long_caches(gpu_device, dtype):
         _check_attention(got, o.attend(codes, scales, q, cu, table, lengths, 0.08), dtype, 64, max(lengths), q)
 
 
+def _attend_heads(case, dtype, scale, window, sinks, heads, rep, hd, picked):
+    """All heads on the GPU, some kv heads in the oracle."""
+    cu, table, lengths, codes, scales, q = case
+    got = _np(_attend(case, dtype, scale, window, sinks))
+    for h in picked:
+        part = slice(h * rep, (h + 1) * rep)
+        want = o.attend(codes[:, h : h + 1], scales[:, h : h + 1], q[:, part], cu, table, lengths, scale, window, sinks)
+        _check_attention(got[:, part], want, dtype, hd, int(lengths.max()), q)
+
+
+@pytest.mark.parametrize("dtype,window,sinks", [("bf16", 0, 0), ("fp16", 200, 5)])
+def test_attention_of_long_chunks(gpu_device, dtype, window, sinks):
+    """More blocks of columns and heads than the chip takes at once; several sequences, one that brings nothing."""
+    rng = np.random.default_rng(18)
+    case = _attend_case(rng, dtype, 16, 8, 64, [100, 7, 0, 300], [700, 0, 301, 150])
+    _attend_heads(case, dtype, 0.07, window, sinks, 16, 8, 64, (0, 15))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attention_of_many_short_chunks(gpu_device, dtype):
+    """More than 256 sequences and blocks of columns, with gaps."""
+    rng = np.random.default_rng(19)
+    news = [int(n) for n in rng.integers(0, 20, 300)]
+    case = _attend_case(rng, dtype, 2, 8, 64, [int(n) for n in rng.integers(0, 90, 300)], news)
+    _attend_heads(case, dtype, 0.07, 0, 0, 2, 8, 64, (1,))
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "fp16"])
 def test_sharp_and_flat_softmax(gpu_device, dtype):
     rng = np.random.default_rng(12)
