@@ -377,80 +377,85 @@ def _dtype(t, what):
 
 
 def _whole(t, what, dtype, shape, device):
-    """A contiguous tensor of that type and shape on that device."""
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    """Address of a contiguous tensor of that type and shape on that device."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous {dtype} {tuple(shape)} on {device} expected, got {t.dtype} "
                          f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
     return t.data_ptr()
 
 
 def _heads(t, what, heads, hd, device, rows=None):
-    """[rows][heads][hd] with neighbouring channels."""
-    if t.dim() != 3 or t.device != device or t.shape[1] != heads or t.shape[2] != hd or t.stride(2) != 1 or (
-            rows is not None and t.shape[0] != rows):
+    """Address, row and head stride of [rows][heads][hd] with neighbouring channels."""
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != hd or t.device != device or (rows is not None and shape[0] != rows):
+        ok = False
+    else:
+        ld, hs, one = t.stride()
+        ok = one == 1
+    if not ok:
         raise ValueError(f"{what}: [{'rows' if rows is None else rows}][{heads}][{hd}] with neighbouring channels on "
-                         f"{device} expected, got {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+                         f"{device} expected, got {tuple(shape)} with strides {t.stride()} on {t.device}")
+    return t.data_ptr(), ld, hs
 
 
-class _On:
-    """The call's device current in this thread, as the entry points want it; nothing to do where it is already."""
+def _at(device, call, *args):
+    """call(*args) with the device current in this thread, as the entry points want it.  (The interpreter's part of a small
+    call is longer than its kernels: this lookup and the one of the stream are the cheap ones.)"""
+    if torch._C._cuda_getDevice() == device.index:
+        return call(*args)
+    with torch.cuda.device(device.index):
+        return call(*args)
 
-    def __init__(self, device):
-        if device.type != "cuda":
-            raise ValueError(f"tensors on a GPU expected, got {device}")
-        self.want = device.index if device.index is not None else torch.cuda.current_device()
 
-    def __enter__(self):
-        self.was = torch.cuda.current_device()
-        if self.was != self.want:
-            torch.cuda.set_device(self.want)
+def _run(device, call, *args):
+    """The call on the device's current stream."""
+    rc = _at(device, call, *args, torch._C._cuda_getCurrentRawStream(device.index))
+    if rc != RVQ_OK:
+        raise RvqError(rc)
 
-    def __exit__(self, *exc):
-        if self.was != self.want:
-            torch.cuda.set_device(self.was)
+
+def _on_gpu(device):
+    if device.type != "cuda":
+        raise ValueError(f"tensors on a GPU expected, got {device}")
+    return device
 
 
 def _tables(cos, sin, rows, device):
-    if (cos is None) != (sin is None):
-        raise ValueError("cos and sin belong together")
-    if cos is None:
+    """Addresses of the tables and the channels that they rotate."""
+    if cos is None or sin is None:
+        if cos is not sin:
+            raise ValueError("cos and sin belong together")
         return None, None, 0
-    half = cos.shape[-1]
-    return (_whole(cos, "cos", torch.float32, (rows, half), device), _whole(sin, "sin", torch.float32, (rows, half), device),
-            2 * half)
+    shape = (rows, cos.shape[-1])
+    return (_whole(cos, "cos", torch.float32, shape, device), _whole(sin, "sin", torch.float32, shape, device), 2 * shape[1])
 
 
 def rope_tables(positions, rot, base=10000.0, factor=1.0, orig_len=0.0, alpha=1.0, beta=32.0, amplitude=1.0, out=None):
     """cos, sin, fp32 [N][rot / 2], of int64 positions [N] (rvq_rope_tables); out: a pair of such tensors."""
-    N, dev = positions.numel(), positions.device
-    p = _whole(positions, "positions", torch.int64, (N,), dev)
-    with _On(dev):
-        if out is None:
-            both = torch.empty((2, N, max(rot, 0) // 2), dtype=torch.float32, device=dev)
-            out = both[0], both[1]
-        cos, sin = out
-        c, s = (_whole(t, "out", torch.float32, (N, max(rot, 0) // 2), dev) for t in out)
-        _chk(lib.rvq_rope_tables(p, N, rot, base, factor, orig_len, alpha, beta, amplitude, c, s, _stream(None)), None)
+    dev = _on_gpu(positions.device)
+    shape = (positions.numel(), max(rot, 0) // 2)
+    p = _whole(positions, "positions", torch.int64, shape[:1], dev)
+    cos, sin = out if out is not None else torch.empty((2, *shape), dtype=torch.float32, device=dev).unbind()
+    _run(dev, lib.rvq_rope_tables, p, shape[0], rot, base, factor, orig_len, alpha, beta, amplitude,
+         _whole(cos, "out", torch.float32, shape, dev), _whole(sin, "out", torch.float32, shape, dev))
     return cos, sin
 
 
 def rope(x, cos, sin, layout=ROPE_ADJACENT, out=None):
     """Head vectors x [N][heads][head_dim] with the first 2 * cos.shape[1] channels of each rotated (rvq_rope).
     out: a tensor like x, x itself to rotate in place; rows and heads may be strided in both."""
-    dtype, dev = _dtype(x, "x"), x.device
+    dtype, dev = _dtype(x, "x"), _on_gpu(x.device)
     if x.dim() != 3:
         raise ValueError(f"x: [rows][heads][head_dim] expected, got {tuple(x.shape)}")
     N, heads, hd = x.shape
     px, ldx, hsx = _heads(x, "x", heads, hd, dev)
     c, s, rot = _tables(cos, sin, N, dev)
-    with _On(dev):
-        if out is None:
-            out = torch.empty((N, heads, hd), dtype=x.dtype, device=dev)
-        if out.dtype != x.dtype:
-            raise ValueError(f"out: {x.dtype} expected, got {out.dtype}")
-        po, ldo, hso = _heads(out, "out", heads, hd, dev, N)
-        _chk(lib.rvq_rope(px, dtype, N, heads, hd, rot, layout, ldx, hsx, c, s, po, ldo, hso, _stream(None)), None)
+    if out is None:
+        out = torch.empty((N, heads, hd), dtype=x.dtype, device=dev)
+    elif out.dtype != x.dtype:
+        raise ValueError(f"out: {x.dtype} expected, got {out.dtype}")
+    po, ldo, hso = _heads(out, "out", heads, hd, dev, N)
+    _run(dev, lib.rvq_rope, px, dtype, N, heads, hd, rot, layout, ldx, hsx, c, s, po, ldo, hso)
     return out
 
 
@@ -463,14 +468,15 @@ class Cache8:
     replayed with other lengths and pages.  Which pages are free is the caller's business."""
 
     def __init__(self, pages, scales):
-        if pages.dim() != 4 or pages.shape[2] != 2 or pages.shape[3] % PAGE_TOKENS:
-            raise ValueError(f"pages: [n_pages][n_kv_heads][2][{PAGE_TOKENS} * head_dim] expected, got {tuple(pages.shape)}")
+        shape = pages.shape
+        if len(shape) != 4 or shape[2] != 2 or shape[3] % PAGE_TOKENS:
+            raise ValueError(f"pages: [n_pages][n_kv_heads][2][{PAGE_TOKENS} * head_dim] expected, got {tuple(shape)}")
         self.device = pages.device
-        self.n_pages, self.n_kv_heads, self.head_dim = pages.shape[0], pages.shape[1], pages.shape[3] // PAGE_TOKENS
-        p = _whole(pages, "pages", torch.uint8, pages.shape, self.device)
-        s = _whole(scales, "scales", torch.float32, pages.shape[:3], self.device)
+        self.n_pages, self.n_kv_heads, _, size = shape
+        self.head_dim = size // PAGE_TOKENS
         self.pages, self.scales = pages, scales
-        self._pool = p, s, self.n_pages, self.n_kv_heads, self.head_dim
+        self._pool = (_whole(pages, "pages", torch.uint8, shape, self.device),
+                      _whole(scales, "scales", torch.float32, shape[:3], self.device), self.n_pages, self.n_kv_heads, self.head_dim)
 
     @classmethod
     def empty(cls, n_pages, n_kv_heads, head_dim, device="cuda"):
@@ -478,69 +484,66 @@ class Cache8:
         return cls(torch.zeros(shape, dtype=torch.uint8, device=device), torch.zeros(shape[:3], dtype=torch.float32, device=device))
 
     def _step(self, cu, table, lengths):
-        n = lengths.shape[0] if lengths.dim() == 1 else -1
-        if table.dim() != 2:
-            raise ValueError(f"table: [sequences][entries] expected, got {tuple(table.shape)}")
-        view = rvq_cache8(*self._pool, _whole(table, "table", torch.int32, (n, table.shape[1]), self.device), table.shape[1], n,
-                          _whole(lengths, "lengths", torch.int32, (n,), self.device))
-        return ctypes.byref(view), _whole(cu, "cu", torch.int32, (n + 1,), self.device)
+        dev = _on_gpu(self.device)
+        shape = table.shape
+        if len(shape) != 2:
+            raise ValueError(f"table: [sequences][entries] expected, got {tuple(shape)}")
+        n = shape[0]
+        view = rvq_cache8(*self._pool, _whole(table, "table", torch.int32, shape, dev), shape[1], n,
+                          _whole(lengths, "lengths", torch.int32, (n,), dev))
+        return view, _whole(cu, "cu", torch.int32, (n + 1,), dev)
 
     def append(self, k, v, cu, table, lengths, cos=None, sin=None, layout=ROPE_ADJACENT):
         """Stores the step's keys, rotated when tables are given, and values, [rows][n_kv_heads][head_dim] (rvq_cache8_append)."""
-        view, pcu = self._step(cu, table, lengths)
-        dtype, rows = _dtype(k, "k"), k.shape[0]
+        dtype, rows, dev = _dtype(k, "k"), k.shape[0], self.device
         if v.dtype != k.dtype:
             raise ValueError(f"v: {k.dtype} expected, got {v.dtype}")
-        pk, ldk, hsk = _heads(k, "k", self.n_kv_heads, self.head_dim, self.device)
-        pv, ldv, hsv = _heads(v, "v", self.n_kv_heads, self.head_dim, self.device, rows)
-        c, s, rot = _tables(cos, sin, rows, self.device)
-        with _On(self.device):
-            _chk(lib.rvq_cache8_append(view, pk, pv, dtype, rows, ldk, hsk, ldv, hsv, pcu, c, s, rot, layout, _stream(None)), None)
+        view, pcu = self._step(cu, table, lengths)
+        pk, ldk, hsk = _heads(k, "k", self.n_kv_heads, self.head_dim, dev)
+        pv, ldv, hsv = _heads(v, "v", self.n_kv_heads, self.head_dim, dev, rows)
+        c, s, rot = _tables(cos, sin, rows, dev)
+        _run(dev, lib.rvq_cache8_append, view, pk, pv, dtype, rows, ldk, hsk, ldv, hsv, pcu, c, s, rot, layout)
 
     def read(self, rows, cu, first, table, lengths, dtype=torch.float16, cos=None, sin=None, layout=ROPE_ADJACENT, out=None):
         """k, v [rows][n_kv_heads][head_dim]: row cu[b] + i is the token of sequence b at position first[b] + i; with
         tables, keys as they were before the rotation (rvq_cache8_read).  out: a pair of such tensors."""
+        dev = self.device
         view, pcu = self._step(cu, table, lengths)
-        pf = _whole(first, "first", torch.int32, lengths.shape, self.device)
-        c, s, rot = _tables(cos, sin, rows, self.device)
-        with _On(self.device):
-            if out is None:
-                both = torch.empty((2, rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
-                out = both[0], both[1]
-            k, v = out
-            code = _dtype(k, "out")
-            if v.dtype != k.dtype:
-                raise ValueError(f"out: one type expected, got {k.dtype} and {v.dtype}")
-            pk, ldk, hsk = _heads(k, "out", self.n_kv_heads, self.head_dim, self.device, rows)
-            pv, ldv, hsv = _heads(v, "out", self.n_kv_heads, self.head_dim, self.device, rows)
-            _chk(lib.rvq_cache8_read(view, pcu, pf, rows, c, s, rot, layout, code, pk, ldk, hsk, pv, ldv, hsv, _stream(None)), None)
+        pf = _whole(first, "first", torch.int32, lengths.shape, dev)
+        c, s, rot = _tables(cos, sin, rows, dev)
+        if out is None:
+            out = torch.empty((2, rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=dev).unbind()
+        k, v = out
+        code = _dtype(k, "out")
+        if v.dtype != k.dtype:
+            raise ValueError(f"out: one type expected, got {k.dtype} and {v.dtype}")
+        pk, ldk, hsk = _heads(k, "out", self.n_kv_heads, self.head_dim, dev, rows)
+        pv, ldv, hsv = _heads(v, "out", self.n_kv_heads, self.head_dim, dev, rows)
+        _run(dev, lib.rvq_cache8_read, view, pcu, pf, rows, c, s, rot, layout, code, pk, ldk, hsk, pv, ldv, hsv)
         return k, v
 
-    def workspace_bytes(self, q):
-        """Bytes of workspace that attend() needs for queries of that shape and type."""
-        with _On(self.device):
-            view = rvq_cache8(*self._pool, None, 1, 1, None)  # the size does not depend on the sequences
-            return lib.rvq_cache8_attn_workspace_bytes(ctypes.byref(view), _dtype(q, "q"), q.shape[0], q.shape[1])
+    def workspace_bytes(self, q, n_seqs):
+        """Bytes of workspace that attend() needs for queries of that shape and type from so many sequences."""
+        view = rvq_cache8(*self._pool, None, 1, n_seqs, None)  # the rest of the step does not matter
+        return _at(_on_gpu(self.device), lib.rvq_cache8_attn_workspace_bytes, view, _dtype(q, "q"), q.shape[0], q.shape[1])
 
     def attend(self, q, cu, table, lengths, scale=None, window=0, sinks=0, out=None, workspace=None):
-        """Attention of the step's query tokens q [rows][heads][head_dim], already rotated, over the cache
-        (rvq_cache8_attn).  scale: 1 / sqrt(head_dim) if not given; workspace: uint8 of workspace_bytes(q), allocated if not given."""
-        view, pcu = self._step(cu, table, lengths)
-        dtype = _dtype(q, "q")
+        """Attention of the step's query tokens q [rows][heads][head_dim], already rotated, over the cache (rvq_cache8_attn).
+        scale: 1 / sqrt(head_dim) if not given; workspace: uint8, at least workspace_bytes(), allocated if not given."""
+        dtype, dev = _dtype(q, "q"), self.device
         if q.dim() != 3:
             raise ValueError(f"q: [rows][heads][head_dim] expected, got {tuple(q.shape)}")
+        view, pcu = self._step(cu, table, lengths)
         rows, heads, hd = q.shape
-        pq, ldq, hsq = _heads(q, "q", heads, self.head_dim, self.device)
-        with _On(self.device):
-            if out is None:
-                out = torch.empty((rows, heads, hd), dtype=q.dtype, device=self.device)
-            if out.dtype != q.dtype:
-                raise ValueError(f"out: {q.dtype} expected, got {out.dtype}")
-            po, ldo, hso = _heads(out, "out", heads, hd, self.device, rows)
-            if workspace is None:
-                need = lib.rvq_cache8_attn_workspace_bytes(view, dtype, rows, heads)
-                workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-            pw = _whole(workspace, "workspace", torch.uint8, workspace.shape, self.device)
-            _chk(lib.rvq_cache8_attn(view, pq, dtype, rows, heads, ldq, hsq, pcu, scale if scale is not None else hd**-0.5, window,
-                                     sinks, po, ldo, hso, pw, workspace.numel(), _stream(None)), None)
+        pq, ldq, hsq = _heads(q, "q", heads, self.head_dim, dev)
+        if out is None:
+            out = torch.empty((rows, heads, hd), dtype=q.dtype, device=dev)
+        elif out.dtype != q.dtype:
+            raise ValueError(f"out: {q.dtype} expected, got {out.dtype}")
+        po, ldo, hso = _heads(out, "out", heads, hd, dev, rows)
+        if workspace is None:
+            workspace = torch.empty(self.workspace_bytes(q, view.n_seqs), dtype=torch.uint8, device=dev)
+        pw = _whole(workspace, "workspace", torch.uint8, workspace.shape, dev)
+        _run(dev, lib.rvq_cache8_attn, view, pq, dtype, rows, heads, ldq, hsq, pcu, scale if scale is not None else hd**-0.5,
+             window, sinks, po, ldo, hso, pw, workspace.numel())
         return out

@@ -590,7 +590,7 @@ def test_captured_steps_are_replayed_with_other_lengths_and_pages(gpu_device):
         loop.check(step, q, out)
         step = loop.inputs([1, 1, 1])
         d = loop.device(step)
-        ws = torch.empty(loop.cache.workspace_bytes(d["q"]), dtype=torch.uint8, device="cuda")
+        ws = torch.empty(loop.cache.workspace_bytes(d["q"], 3), dtype=torch.uint8, device="cuda")
         q, out = loop.run(d, workspace=ws)
         loop.check(step, q, out)
         pages, scales = loop.cache.pages.clone(), loop.cache.scales.clone()
@@ -660,7 +660,7 @@ def test_a_workspace_that_is_too_small_is_refused(gpu_device):
     cu, table, lengths, codes, scales, q = case
     cache = b.Cache8(_dev(codes), _dev(scales.astype(np.float32)))
     dq = _dev(q, _type("bf16"))
-    need = cache.workspace_bytes(dq)
+    need = cache.workspace_bytes(dq, 1)
     out = torch.full_like(dq, 3.0)
     with pytest.raises(b.RvqError) as e:
         cache.attend(dq, _i32(cu), _i32(table), _i32(lengths), out=out, workspace=torch.empty(need - 16, dtype=torch.uint8, device="cuda"))
