@@ -3,10 +3,7 @@
 
 #include "rvq_rows.h"
 
-namespace {
-
-constexpr int PAGE = RVQ_PAGE_TOKENS;
-
+// what a kernel is given of a cache and of a step
 struct CacheView {
   uint8_t *pages;
   float *scales;
@@ -14,6 +11,11 @@ struct CacheView {
   int64_t n_pages, rows;
   int heads, hd, table_pages, n_seqs;
 };
+
+namespace {
+
+constexpr int PAGE = RVQ_PAGE_TOKENS;
+
 
 // rows of sequence b in this step; whatever the array holds, they lie inside [0, rows)
 struct SeqRows {
@@ -28,9 +30,9 @@ __device__ __forceinline__ SeqRows rows_of(const CacheView &c, int b) {
 }
 
 // the page behind an entry of a sequence's table, or -1: there is none
-__device__ __forceinline__ int64_t page_of(const CacheView &c, int b, int64_t entry) {
+__device__ __forceinline__ int page_of(const CacheView &c, int b, int64_t entry) {
   if (entry < 0 || entry >= c.table_pages) return -1;
-  const int64_t id = c.table[(int64_t)b * c.table_pages + entry];
+  const int id = c.table[(int64_t)b * c.table_pages + entry];
   return id >= 0 && id < c.n_pages ? id : -1;
 }
 
