@@ -6,8 +6,9 @@
 // column and, of the two tiles of 32 tokens, the tokens 32 h .. 32 h + 31 (h = lane / 32): its weights are again what the
 // second product takes from it.
 //
-// What bounds it is the vector pipe: per page and wavefront 32 matrix instructions of 32 clocks stand against 128 conversions
-// and some 8 operations, one of them an exponential, for each of a lane's 32 scores.  So the maximum that weights
+// The keys' codes go to the products as they are, against queries split into e4m3 terms.
+// What bounds it is the vector pipe: per page and wavefront 1024 clocks of matrix instructions stand against 64 conversions
+// and some 4 operations, one of them an exponential of four times the length, for each of a lane's 32 scores.  So the maximum that weights
 // refer to moves only when a score passes it by more than 2^7 (the accumulators are not touched otherwise), weights being
 // held as 2^8 2^(s - m) in fp16: at most 2^15, exact to 11 bits down to 2^-22 of the largest.
 
@@ -16,14 +17,18 @@
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr float CHUNK_BITS = 8.0f, CHUNK_SLACK = 7.0f;
 
-// Units (pages) of all items, or, with FIND, the block and place of unit `target`.  256 blocks per trip: their sequence
-// by bisection of the sequences' prefix sums in LDS, then a prefix sum of their units.
-struct WalkShared {
+// The blocks of all sequences, 256 per trip, one per thread: visit(sequence, block, pages), pages = 0 for none, is called by all
+// threads together until it returns true in all of them.  A block's sequence is found by bisection of the sequences' prefix sums.
+struct Shared {
   int64_t before[257], wave[4];
-  int64_t found[4];
+  int found[3];
+  int64_t rest;
+  int pages_like[512];
+  int flags[WAVES];
 };
 __device__ __forceinline__ int64_t scan256(int64_t x, int64_t *wave, int64_t &total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -45,50 +50,111 @@ __device__ __forceinline__ int64_t scan256(int64_t x, int64_t *wave, int64_t &to
   }
   return sum + add;
 }
-template <bool FIND> __device__ __forceinline__ int64_t walk(const AttnArgs &a, WalkShared &sh, int64_t target) {
+template <typename Visit> __device__ __forceinline__ void walk(const AttnArgs &a, Shared &sh, Visit visit) {
   const int t = threadIdx.x;
-  int64_t base = 0, total;
-  if (FIND && t == 0) sh.found[0] = -1;
   for (int b0 = 0; b0 < a.c.n_seqs; b0 += 256) {
-    const int64_t upto = scan256(b0 + t < a.c.n_seqs ? blocks_of(a, rows_of(a.c, b0 + t).n, MANY) : 0, sh.wave, total);
+    int64_t blocks;
+    const int64_t upto = scan256(b0 + t < a.c.n_seqs ? blocks_of(a, rows_of(a.c, b0 + t).n, MANY) : 0, sh.wave, blocks);
     sh.before[t + 1] = upto;
     if (t == 0) sh.before[0] = 0;
     __syncthreads();
-    const int64_t blocks = total;
     for (int64_t k0 = 0; k0 < blocks; k0 += 256) {
       const int64_t k = k0 + t;
-      int64_t units = 0, j = 0;
-      int s = 0;
+      int s = 0, j = 0, pages = 0;
       if (k < blocks) {
 #pragma unroll
         for (int d = 128; d; d /= 2)
           if (sh.before[s + d] <= k) s += d;
-        j = k - sh.before[s];
+        j = (int)(k - sh.before[s]);
         const Seq q = seq_of(a, b0 + s);
-        const Block x = block_of(a, q, (int)j * MANY, MANY);
-        units = (int64_t)span_of(a, q, x.first, x.last).pages * a.c.heads;
+        const Block x = block_of(a, q, j * MANY, MANY);
+        pages = span_of(a, q, x.first, x.last).pages;
       }
-      const int64_t sum = scan256(units, sh.wave, total);
-      if (FIND) {
-        const int64_t at = base + sum - units;
-        if (at <= target && target < at + units) {
-          sh.found[0] = b0 + s;
-          sh.found[1] = j;
-          sh.found[2] = target - at;
-        }
-        __syncthreads();
-        if (sh.found[0] >= 0) return 0;
-      }
-      base += total;
+      if (visit(b0 + s, j, pages)) return;
     }
     __syncthreads();
   }
-  return base;
 }
+
+// pages of all items
+__device__ __forceinline__ int64_t all_units(const AttnArgs &a, Shared &sh) {
+  int64_t mine = 0, total;
+  walk(a, sh, [&](int, int, int pages) {
+    mine += (int64_t)pages * a.c.heads;
+    return false;
+  });
+  (void)scan256(mine, sh.wave, total);
+  return total;
+}
+
+// the block that holds unit `target`, and the unit's place in it: found[0], found[1], rest
+__device__ __forceinline__ void find_unit(const AttnArgs &a, Shared &sh, int64_t target) {
+  int64_t base = 0;
+  if (threadIdx.x == 0) sh.found[0] = -1;
+  walk(a, sh, [&](int b, int j, int pages) {
+    const int64_t units = (int64_t)pages * a.c.heads;
+    int64_t total;
+    const int64_t at = base + scan256(units, sh.wave, total) - units;
+    if (at <= target && target < at + units) {
+      sh.found[0] = b;
+      sh.found[1] = j;
+      sh.rest = target - at;
+    }
+    __syncthreads();
+    base += total;
+    return sh.found[0] >= 0;
+  });
+}
+
+// Blocks by length, the longest first, to within a sixteenth: a block's class is the exponent of its pages and four more bits.
+__device__ __forceinline__ int class_of(int pages) {
+  const int e = 31 - __clz(pages);
+  return 511 - (e * 16 + (int)(((int64_t)pages << 4) >> e) - 16);
+}
+// the block of that rank: found[0], found[1]; found[0] < 0: there are not so many
+__device__ __forceinline__ void find_rank(const AttnArgs &a, Shared &sh, int64_t rank) {
+  const int t = threadIdx.x;
+  sh.pages_like[t] = sh.pages_like[t + 256] = 0;
+  if (t == 0) sh.found[0] = sh.found[2] = -1;
+  walk(a, sh, [&](int, int, int pages) {  // (barriers of the walk come before the first count)
+    if (pages) atomicAdd(&sh.pages_like[class_of(pages)], 1);
+    return false;
+  });
+  __syncthreads();
+  const int two = sh.pages_like[2 * t] + sh.pages_like[2 * t + 1];
+  int64_t total;
+  const int64_t at = scan256(two, sh.wave, total) - two;
+  if (at <= rank && rank < at + two) {
+    const bool second = rank >= at + sh.pages_like[2 * t];
+    sh.found[2] = 2 * t + second;
+    sh.rest = rank - at - (second ? sh.pages_like[2 * t] : 0);
+  }
+  __syncthreads();
+  const int cls = sh.found[2];
+  if (cls < 0) return;
+  const int64_t place = sh.rest;
+  int64_t base = 0;
+  walk(a, sh, [&](int b, int j, int pages) {
+    const int hit = pages && class_of(pages) == cls;
+    const int64_t before = base + scan256(hit, sh.wave, total) - hit;
+    if (hit && before == place) {
+      sh.found[0] = b;
+      sh.found[1] = j;
+    }
+    __syncthreads();
+    base += total;
+    return sh.found[0] >= 0;
+  });
+}
+
+// A query as e4m3 terms for the products with the keys' codes as they are: 4 bits each, the next one 2^-4 of the last, so
+// two hold a bf16 number and three an fp16 one (but for what lies below 2^-21 and 2^-25 of the row's largest element).
+template <typename T> constexpr int TERMS = std::is_same<T, _Float16>::value ? 3 : 2;
 
 template <typename T, int HD> struct Chunk {
   static constexpr int BYTES = 2 * PAGE * HD;  // of a page and kv head
-  f16x8 q[HD / 16];  // product 2 c + i takes channels 32 c + 16 h + 8 i ..
+  static constexpr int STEPS = HD / 64;        // products of 64 channels; a lane holds channels 64 c + 32 h ..
+  i32x8 q[STEPS][TERMS<T>];
   f32x16 acc[HD / 32];
   float factor, m, l;
   Sight sight;
@@ -104,16 +170,16 @@ __device__ __forceinline__ void load_chunk(const AttnArgs &a, const Seq &s, int 
 #pragma unroll
   for (int i = 0; i < HD / 16; ++i) {
     if (valid) {
-      load8<T>(q + (i >> 1) * 32 + h * 16 + (i & 1) * 8, x[i]);
+      load8<T>(q + (i >> 2) * 64 + h * 32 + (i & 3) * 8, x[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(x[i][j]));
+    for (int j = 0; j < 8; ++j) amax = not_finite(x[i][j]) ? __uint_as_float(0x7f800000u) : fmaxf(amax, fabsf(x[i][j]));
   }
   amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
-  int e = (int)(__float_as_uint(amax) >> 23) - 127 - 8;
+  int e = (int)(__float_as_uint(amax) >> 23) - 127 - 7;  // largest element to [2^7, 2^8)
   e = e < -118 ? -118 : e;
   // a factor >= 0, so that the largest product is the largest score; not 0, which would make a number of a hidden one
   const float down = __uint_as_float((uint32_t)(127 - e) << 23) * (a.scale < 0.0f ? -1.0f : 1.0f);
@@ -123,7 +189,17 @@ __device__ __forceinline__ void load_chunk(const AttnArgs &a, const Seq &s, int 
   for (int i = 0; i < HD / 16; ++i) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[i][j] *= down;
-    k.q[i] = half8(x[i]);
+#pragma unroll
+    for (int t = 0; t < TERMS<T>; ++t)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float *v = &x[i][4 * j], was[4];
+        const uint32_t code = amax < __uint_as_float(0x7f800000u) ? encode4(v[0], v[1], v[2], v[3]) : 0x7f7f7f7fu;
+        k.q[i >> 2][t][(i & 3) * 2 + j] = (int)code;
+        decode4(code, was);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = (v[r] - was[r]) * 16.0f;
+      }
   }
 #pragma unroll
   for (int i = 0; i < HD / 32; ++i) k.acc[i] = f32x16{};
@@ -131,30 +207,66 @@ __device__ __forceinline__ void load_chunk(const AttnArgs &a, const Seq &s, int 
   k.l = 0.0f;
 }
 
-// Where 16-byte piece c of a row lies in LDS: rows of keys (HD bytes, HD / 16 pieces) and of values (64 bytes, 4
-// pieces).  A wavefront reads one piece column of 32 rows at a time.
-template <int PIECES> __device__ __forceinline__ int piece(int row, int c) {
-  return PIECES == 4 ? c ^ ((row >> 1) & 3) : c ^ (row & 7);
+// Where 16-byte piece c of a row lies in LDS, for keys (HD bytes a row) and values (64 bytes).  Eight lanes read a piece each
+// per LDS cycle, of rows 0 1 2 3 32 33 34 35 (keys: the order of a tile's tokens) or of eight rows in turn (values); so placed, the
+// eight lie in different banks.
+template <int HD> __device__ __forceinline__ int key_piece(int row, int c) {
+  return HD == 64 ? c ^ (((row >> 1) & 1) | ((row >> 4) & 2)) : c ^ ((row & 3) | ((row >> 3) & 4));
+}
+__device__ __forceinline__ int value_piece(int row, int c) { return c ^ ((row >> 1) & 3); }
+
+// Copies a page's codes of one kv head to LDS, 1024 bytes per wavefront and step, keys first; a wavefront's own part is complete
+// after vmcnt(0).  `from`: this lane's bytes of the page.
+template <int HD> struct Fetch {
+  static constexpr int STEPS = 2 * HD / 64;
+  uint32_t from[STEPS];
+  __device__ __forceinline__ Fetch() {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int at = (i * WAVES + wave) * 64 + lane;  // 16-byte piece in LDS
+      if (i < HD / 64) {
+        const int row = at / (HD / 16);
+        from[i] = (row * (HD / 16) + key_piece<HD>(row, at % (HD / 16))) * 16;
+      } else {
+        const int row = (at - 4 * HD) >> 2;
+        from[i] = (4 * HD + row * 4 + value_piece(row, at & 3)) * 16;
+      }
+    }
+  }
+  __device__ __forceinline__ void operator()(const uint8_t *codes, uint8_t *to) const {
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(codes + from[i]),
+                                       (__attribute__((address_space(3))) void *)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
+  }
+};
+
+// Of the pages of a span, by their place i: those behind the sinks' that a block of columns sees anything of, [from, to), and
+// those that it sees whole, [all_from, all_to).  (Pages of sinks, where there are any, count as seen in part.)
+struct Range {
+  int from, to, all_from, all_to;
+};
+__device__ __forceinline__ Range range_of(const AttnArgs &a, const Seq &s, const Block &k, const Span &span) {
+  const int shift = span.sink_pages - span.begin;  // place = page + shift
+  const int hide = hidden_to(a, k.first), hide_all = hidden_to(a, k.last);
+  const int seen = min(k.last, s.tokens - 1), seen_by_all = min(k.first, s.tokens - 1);
+  Range r;
+  r.from = a.sinks > span.begin * PAGE ? span.sink_pages : max(span.sink_pages, (hide + 1) / PAGE + shift);
+  r.to = (seen < 0 ? 0 : seen / PAGE + 1) + shift;
+  r.all_from = max(span.sink_pages, (hide_all + PAGE) / PAGE + shift);
+  r.all_to = (seen_by_all + 1) / PAGE + shift;
+  return r;
 }
 
-// copies a page's codes of one kv head to LDS; complete for a wavefront's own part after vmcnt(0)
-template <int HD> __device__ __forceinline__ void fetch_page(const uint8_t *codes, uint8_t *to) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int i = 0; i < 2 * HD / 64; ++i) {  // 1024 bytes per wavefront and step, keys first
-    const int at = (i * WAVES + wave) * 64 + lane;  // 16-byte piece in LDS
-    int from;
-    if (i < HD / 64) {
-      const int row = at / (HD / 16), c = at % (HD / 16);
-      from = row * (HD / 16) + piece<HD / 16>(row, c);
-    } else {
-      const int v = at - 4 * HD, row = v >> 2, c = v & 3;
-      from = 4 * HD + row * 4 + piece<4>(row, c);
-    }
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(codes + from * 16),
-                                     (__attribute__((address_space(3))) void *)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
-  }
+// bit i: this lane's column sees token t0 + i, i < 32
+__device__ __forceinline__ uint32_t ones(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t seen_bits(const AttnArgs &a, const Sight &x, int t0) {
+  return ones(x.to - t0 + 1) & (~ones(x.hidden - t0 + 1) | ones(a.sinks - t0));
 }
+// all bits of the result are bit i of x
+__device__ __forceinline__ uint32_t spread_bit(uint32_t x, int i) { return (uint32_t)((int)(x << (31 - i)) >> 31); }
 
 // One page for this wavefront's columns.  `whole`: every column sees every token; values' codes hold no NaN otherwise.
 template <typename T, int HD>
@@ -167,19 +279,24 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
   for (int i = 0; i < 2; ++i) {
     // row n of tile i is token 32 ((n / 4) % 2) + 16 i + 4 (n / 8) + n % 4
     const int row = ((n >> 2) & 1) * 32 + i * 16 + (n >> 3) * 4 + (n & 3);
-    u32x4 x[HD / 32];
-#pragma unroll
-    for (int c = 0; c < HD / 32; ++c) x[c] = *reinterpret_cast<const u32x4 *>(kc + row * HD + piece<HD / 16>(row, 2 * c + h) * 16);
     s[i] = f32x16{};
 #pragma unroll
-    for (int c = 0; c < HD / 32; ++c) {
-      s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(x[c][0], x[c][1]), k.q[2 * c], s[i], 0, 0, 0);
-      s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(x[c][2], x[c][3]), k.q[2 * c + 1], s[i], 0, 0, 0);
+    for (int c = 0; c < HD / 64; ++c) {
+      const u32x4 lo = *reinterpret_cast<const u32x4 *>(kc + row * HD + key_piece<HD>(row, 4 * c + 2 * h) * 16);
+      const u32x4 hi = *reinterpret_cast<const u32x4 *>(kc + row * HD + key_piece<HD>(row, 4 * c + 2 * h + 1) * 16);
+      const i32x8 x = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+#pragma unroll
+      for (int t = 0; t < TERMS<T>; ++t)  // the operands' block scales: 1, and 2^-4 for each further term
+        s[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, k.q[c][t], s[i], 0, 0, 0, 127, 0, 127 - 4 * t);
     }
   }
   if (!whole) {
+    const uint32_t seen = seen_bits(a, k.sight, t0 + h * 32);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = sees(a, k.sight, t0 + h * 32 + i) ? s[i >> 4][i & 15] : -INFINITY;
+    for (int i = 0; i < 32; ++i) {
+      const uint32_t m = spread_bit(seen, i);
+      s[i >> 4][i & 15] = __uint_as_float((__float_as_uint(s[i >> 4][i & 15]) & m) | (0xff800000u & ~m));  // hidden: -infinity
+    }
   }
   float top = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
@@ -207,31 +324,26 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
     count = unit / vscale;
     ref -= __builtin_amdgcn_logf(count);
   }
-  float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      s[i][j] = __builtin_amdgcn_exp2f(fmaf(s[i][j], factor, ref));
-      sum[i] += s[i][j];
-    }
-  k.l += (sum[0] + sum[1]) * count;
   f16x8 w[4];
+  float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const f32x2 two = {s[i >> 1][(i & 1) * 8 + 2 * j], s[i >> 1][(i & 1) * 8 + 2 * j + 1]};
+      const int at = (i & 1) * 8 + 2 * j;
+      const f32x2 two = {__builtin_amdgcn_exp2f(fmaf(s[i >> 1][at], factor, ref)), __builtin_amdgcn_exp2f(fmaf(s[i >> 1][at + 1], factor, ref))};
       const f16x2 r = __builtin_convertvector(two, f16x2);
+      sum = __builtin_amdgcn_fdot2(r, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
       w[i][2 * j] = r[0];
       w[i][2 * j + 1] = r[1];
     }
+  k.l += sum * count;
 #pragma unroll
   for (int c = 0; c < HD / 32; ++c) {
     const int row = c * 32 + n;
     u32x4 v[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const u32x4 *>(vc + row * PAGE + piece<4>(row, 2 * h + i) * 16);
+    for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const u32x4 *>(vc + row * PAGE + value_piece(row, 2 * h + i) * 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       k.acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(v[i >> 1][(i & 1) * 2], v[i >> 1][(i & 1) * 2 + 1]), w[i], k.acc[c], 0, 0, 0);
@@ -255,18 +367,21 @@ __device__ __forceinline__ void settle_nan(const AttnArgs &a, Chunk<T, HD> &k, u
   __syncthreads();
   if (!__builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3])) return;
   if (busy) {
+    const uint32_t seen = seen_bits(a, k.sight, t0 + h * 32);
 #pragma unroll
     for (int c = 0; c < HD / 32; ++c) {
       const int row = c * 32 + n;
       f32x16 d = f32x16{};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const u32x2 v = *reinterpret_cast<const u32x2 *>(vc + row * PAGE + piece<4>(row, 2 * h + (i >> 1)) * 16 + (i & 1) * 8);
-        f16x8 one;
+        const u32x2 v = *reinterpret_cast<const u32x2 *>(vc + row * PAGE + value_piece(row, 2 * h + (i >> 1)) * 16 + (i & 1) * 8);
+        u32x4 one;  // fp16 ones of the tokens that are seen
 #pragma unroll
-        for (int j = 0; j < 8; ++j) one[j] = sees(a, k.sight, t0 + h * 32 + i * 8 + j) ? (_Float16)1.0f : (_Float16)0.0f;
+        for (int j = 0; j < 4; ++j)
+          one[j] = (spread_bit(seen, i * 8 + 2 * j) & 0x3c00u) | (spread_bit(seen, i * 8 + 2 * j + 1) & 0x3c000000u);
         // 0x38 is the code of 1
-        d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8((nan_bytes(v[0]) >> 7) * 0x38u, (nan_bytes(v[1]) >> 7) * 0x38u), one, d, 0, 0, 0);
+        d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8((nan_bytes(v[0]) >> 7) * 0x38u, (nan_bytes(v[1]) >> 7) * 0x38u),
+                                                   __builtin_bit_cast(f16x8, one), d, 0, 0, 0);
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) k.acc[c][r] = d[r] > 0.0f ? __uint_as_float(0x7fc00000u) : k.acc[c][r];
@@ -284,44 +399,45 @@ __device__ __forceinline__ void settle_nan(const AttnArgs &a, Chunk<T, HD> &k, u
   __syncthreads();
 }
 
-// `whole`: a workgroup takes one item, blockIdx.x / heads counting blocks from the last of every sequence (the longest) on;
-// else an equal run of the items' pages, as in the kernel for few columns.
+// whole_items: a workgroup takes one item, the longest first (in the order of the blocks, three sequences of 2000 to 2500 tokens
+// behind 1000 to 3300 keep the chip busy for 237 pages' time, longest first 215, of 206 that all the work takes); else an equal run of the items' pages, as in the kernel for few columns.
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_kernel(const AttnArgs a, int whole_items) {
   typedef Chunk<T, HD> C;
   __shared__ __align__(16) uint8_t tile[2][C::BYTES];
-  __shared__ WalkShared sh;
-  __shared__ int flags[WAVES];
+  __shared__ Shared sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
   const int64_t w = blockIdx.x;
   int b, head, j, x = 0;
   int64_t left, run = 1;
   if (whole_items) {
-    int64_t at;
-    if (!find_piece(a.c.n_seqs, w / a.c.heads, [&](int i) { return (int64_t)blocks_of(a, rows_of(a.c, i).n, MANY); }, b, at)) return;
+    find_rank(a, sh, w / a.c.heads);
+    if (sh.found[0] < 0) return;
+    b = sh.found[0];
+    j = sh.found[1];
     head = (int)(w % a.c.heads);
-    j = blocks_of(a, rows_of(a.c, b).n, MANY) - 1 - (int)at;
     left = INT32_MAX;
   } else {
     if (threadIdx.x == 0) a.header[w * 8 + H_PARTS] = 0;
-    const int64_t total = walk<false>(a, sh, 0), even = (total + gridDim.x - 1) / gridDim.x;
+    const int64_t total = all_units(a, sh), even = (total + gridDim.x - 1) / gridDim.x;
     run = even > a.least ? even : a.least;
     if (w * run >= total) return;
-    walk<true>(a, sh, w * run);
-    b = (int)sh.found[0];
-    j = (int)sh.found[1];
+    find_unit(a, sh, w * run);
+    b = sh.found[0];
+    j = sh.found[1];
     left = run;
     const Seq s = seq_of(a, b);
     const Block k = block_of(a, s, j * MANY, MANY);
     const int pages = span_of(a, s, k.first, k.last).pages;
-    head = (int)(sh.found[2] / pages);
-    x = (int)(sh.found[2] % pages);
+    head = (int)(sh.rest / pages);
+    x = (int)(sh.rest % pages);
   }
   b = __builtin_amdgcn_readfirstlane(b);
   head = __builtin_amdgcn_readfirstlane(head);
   j = __builtin_amdgcn_readfirstlane(j);
   x = __builtin_amdgcn_readfirstlane(x);
   bool at_start = true;
+  const Fetch<HD> fetch;
   while (true) {
     const Seq s = seq_of(a, b);
     const Block k = block_of(a, s, j * MANY, MANY);
@@ -334,27 +450,39 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
     float unit = 1.0f;  // scale of the accumulators, the same in every lane
     // this wavefront's columns
     const bool busy = wave * 32 < k.cols;
-    const Block mine = busy ? block_of(a, s, k.col0 + wave * 32, min(32, k.cols - wave * 32)) : k;
+    const Range mine = range_of(a, s, busy ? block_of(a, s, k.col0 + wave * 32, min(32, k.cols - wave * 32)) : k, span);
+    const Range ours = range_of(a, s, k, span);
+    const int m_from = __builtin_amdgcn_readfirstlane(mine.from), m_to = __builtin_amdgcn_readfirstlane(busy ? mine.to : 0);
+    const int m_all_from = __builtin_amdgcn_readfirstlane(mine.all_from), m_all_to = __builtin_amdgcn_readfirstlane(mine.all_to);
     // the page in hand, the next one, on its way to LDS while the wavefronts work on this, and the entry behind it
-    const auto scales_of = [&](int id) { return id >= 0 ? *reinterpret_cast<const f32x2 *>(scale_of(a.c, id, head, 0)) : f32x2{0, 0}; };
-    int page = __builtin_amdgcn_readfirstlane(page_of(a.c, b, span.entry(x)));
-    int next = x + 1 < end ? page_of(a.c, b, span.entry(x + 1)) : -1;
+    const int32_t *table = a.c.table + (int64_t)b * a.c.table_pages;
+    const uint8_t *codes = codes_of(a.c, 0, head, 0);
+    const float *scale = scale_of(a.c, 0, head, 0);
+    const int64_t page_bytes = (int64_t)a.c.heads * C::BYTES;
+    const int n_pages = (int)min(a.c.n_pages, (int64_t)INT32_MAX), sinks = span.sink_pages, behind = span.begin - sinks;
+    const auto id_of = [&](int i) {
+      const int entry = i < sinks ? i : i + behind;
+      const int id = i < end && entry < a.c.table_pages ? table[entry] : -1;
+      return id < n_pages ? id : -1;
+    };
+    const auto scales_of = [&](int id) { return *reinterpret_cast<const f32x2 *>(scale + (int64_t)max(id, 0) * a.c.heads * 2); };
+    int page = __builtin_amdgcn_readfirstlane(id_of(x)), next = id_of(x + 1);
     f32x2 scales = scales_of(page);
     __syncthreads();  // the tiles are free
-    if (page >= 0) fetch_page<HD>(codes_of(a.c, page, head, 0), tile[0]);
+    if (page >= 0) fetch(codes + page * page_bytes, tile[0]);
     for (int i = x; i < end; ++i) {
       const int cur = (i - x) & 1;
       __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wavefront's part of the page has landed
       __syncthreads();
       next = __builtin_amdgcn_readfirstlane(next);
-      const int after = i + 2 < end ? page_of(a.c, b, span.entry(i + 2)) : -1;
+      const int after = id_of(i + 2);
       const f32x2 next_scales = scales_of(next);
-      if (next >= 0) fetch_page<HD>(codes_of(a.c, next, head, 0), tile[cur ^ 1]);
-      const int t0 = span.entry(i) * PAGE;
+      if (next >= 0) fetch(codes + next * page_bytes, tile[cur ^ 1]);
       if (page >= 0) {
-        if (!all_see(a, s, k, t0)) settle_nan<T, HD>(a, c, tile[cur] + PAGE * HD, t0, busy, flags);
-        if (busy && !none_sees(a, s, mine, t0))
-          take_chunk_page<T, HD>(a, c, tile[cur], uniform(scales[0]), uniform(scales[1]), unit, t0, all_see(a, s, mine, t0));
+        const int t0 = (i < sinks ? i : i + behind) * PAGE;
+        if (i < ours.all_from || i >= ours.all_to) settle_nan<T, HD>(a, c, tile[cur] + PAGE * HD, t0, busy, sh.flags);
+        if (i < m_to && (i >= m_from || i < sinks))
+          take_chunk_page<T, HD>(a, c, tile[cur], uniform(scales[0]), uniform(scales[1]), unit, t0, i >= m_all_from && i < m_all_to);
       }
       page = next;
       next = after;
