@@ -19,7 +19,7 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-constexpr float CHUNK_BITS = 8.0f, CHUNK_SLACK = 7.0f;
+constexpr float CHUNK_BITS = 8.0f;  // weights are held as 2^8 2^(s - m)
 
 // The blocks of all sequences, 256 per trip, one per thread: visit(sequence, block, pages), pages = 0 for none, is called by all
 // threads together until it returns true in all of them.  A block's sequence is found by bisection of the sequences' prefix sums.
@@ -290,6 +290,16 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
         s[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, k.q[c][t], s[i], 0, 0, 0, 127, 0, 127 - 4 * t);
     }
   }
+  // the values' codes are on their way while the weights are made
+  u32x4 v[HD / 32][2];
+#pragma unroll
+  for (int c = 0; c < HD / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = c * 32 + n;
+      v[c][i] = *reinterpret_cast<const u32x4 *>(vc + row * PAGE + value_piece(row, 2 * h + i) * 16);
+    }
+  __builtin_amdgcn_sched_barrier(0);
   if (!whole) {
     const uint32_t seen = seen_bits(a, k.sight, t0 + h * 32);
 #pragma unroll
@@ -298,56 +308,61 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
       s[i >> 4][i & 15] = __uint_as_float((__float_as_uint(s[i >> 4][i & 15]) & m) | (0xff800000u & ~m));  // hidden: -infinity
     }
   }
-  float top = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-  for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
-  top = fmaxf(top, __shfl_xor(top, 32, 64));
   const float factor = k.factor * kscale;
-  top = fmaxf(k.m, top * factor);
-  // (the condition is the same in every lane; it is handed over as a scalar so that the branch leaves the accumulators in place)
-  const int move = (__ballot(top > k.m + CHUNK_SLACK) != 0) | (vscale > unit) | (vscale < unit * 0x1p-6f);
-  if (__builtin_amdgcn_readfirstlane(move)) {
-    // the accumulators' unit: this page's scale, but no more than 2^40 below the last one
-    const float low = unit * 0x1p-40f, to = uniform(vscale < low ? low : vscale);
-    const float fix = __builtin_amdgcn_exp2f(k.m - top), all = fix * (unit / to);
-    k.m = top;
-    k.l *= fix;
+  // a page of a smaller scale than the accumulators' unit: its weights are that much smaller, but not in the sum of weights
+  if (__builtin_amdgcn_readfirstlane((vscale > unit) | (vscale < unit * 0x1p-6f))) {
+    // a larger scale, or a much smaller one, becomes the unit (by at most 2^40 downwards at a time)
+    const float low = unit * 0x1p-40f, to = uniform(vscale < low ? low : vscale), all = unit / to;
     unit = to;
 #pragma unroll
     for (int c = 0; c < HD / 32; ++c)
 #pragma unroll
       for (int r = 0; r < 16; ++r) k.acc[c][r] *= all;
   }
-  // a page of a smaller scale than the accumulators' unit: its weights are that much smaller, but not in the sum of weights
-  float ref = CHUNK_BITS - k.m, count = 1.0f;
+  float shift = CHUNK_BITS, count = 1.0f;
   if (vscale != unit) {
     count = unit / vscale;
-    ref -= __builtin_amdgcn_logf(count);
+    shift -= __builtin_amdgcn_logf(count);
   }
   f16x8 w[4];
-  float sum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int at = (i & 1) * 8 + 2 * j;
-      const f32x2 two = {__builtin_amdgcn_exp2f(fmaf(s[i >> 1][at], factor, ref)), __builtin_amdgcn_exp2f(fmaf(s[i >> 1][at + 1], factor, ref))};
-      const f16x2 r = __builtin_convertvector(two, f16x2);
-      sum = __builtin_amdgcn_fdot2(r, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
-      w[i][2 * j] = r[0];
-      w[i][2 * j + 1] = r[1];
-    }
-  k.l += sum * count;
-#pragma unroll
-  for (int c = 0; c < HD / 32; ++c) {
-    const int row = c * 32 + n;
-    u32x4 v[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const u32x4 *>(vc + row * PAGE + value_piece(row, 2 * h + i) * 16);
+  float sum;
+  const auto weigh = [&](float ref) {
+    sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      k.acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(v[i >> 1][(i & 1) * 2], v[i >> 1][(i & 1) * 2 + 1]), w[i], k.acc[c], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = (i & 1) * 8 + 2 * j;
+        const f32x2 two = {__builtin_amdgcn_exp2f(fmaf(s[i >> 1][at], factor, ref)), __builtin_amdgcn_exp2f(fmaf(s[i >> 1][at + 1], factor, ref))};
+        const f16x2 r = __builtin_convertvector(two, f16x2);
+        sum = __builtin_amdgcn_fdot2(r, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+        w[i][2 * j] = r[0];
+        w[i][2 * j + 1] = r[1];
+      }
+  };
+  weigh(shift - k.m);
+  // A weight beyond fp16 (infinity in the sum) asks for another reference: the maximum so far.
+  if (__builtin_amdgcn_readfirstlane(__ballot(sum == INFINITY) != 0)) {
+    float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    top = fmaxf(k.m, top * factor);
+    const float fix = __builtin_amdgcn_exp2f(k.m - top);
+    k.m = top;
+    k.l *= fix;
+#pragma unroll
+    for (int c = 0; c < HD / 32; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) k.acc[c][r] *= fix;
+    weigh(shift - k.m);
   }
+  k.l += sum * count;
+#pragma unroll
+  for (int c = 0; c < HD / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      k.acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(v[c][i >> 1][(i & 1) * 2], v[c][i >> 1][(i & 1) * 2 + 1]), w[i], k.acc[c], 0, 0, 0);
 }
 
 // A NaN among the values' codes of a slot that some column does not see must not meet its weight of 0.  For pages that not
