@@ -82,7 +82,13 @@ struct Sight {
 __device__ __forceinline__ Sight sight_of(const AttnArgs &a, const Seq &s, int p) {
   return {p < s.tokens - 1 ? p : s.tokens - 1, hidden_to(a, p)};
 }
-__device__ __forceinline__ bool sees(const AttnArgs &a, const Sight &x, int t) { return t <= x.to && (t > x.hidden || t < a.sinks); }
+// bit i: this lane's column sees token t0 + i, i < 32
+__device__ __forceinline__ uint32_t ones(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t seen_bits(const AttnArgs &a, const Sight &x, int t0) {
+  return ones(x.to - t0 + 1) & (~ones(x.hidden - t0 + 1) | ones(a.sinks - t0));
+}
+// all bits of the result are bit i of x
+__device__ __forceinline__ uint32_t spread_bit(uint32_t x, int i) { return (uint32_t)((int)(x << (31 - i)) >> 31); }
 // none or all of the page at t0 is seen by all columns of a block
 __device__ __forceinline__ bool none_sees(const AttnArgs &a, const Seq &s, const Block &k, int t0) {
   return t0 > k.last || t0 >= s.tokens || (t0 + PAGE - 1 <= hidden_to(a, k.first) && t0 >= a.sinks);

@@ -38,15 +38,39 @@ __device__ __forceinline__ int64_t units_of(const AttnArgs &a, int b) {
   return (int64_t)blocks_of(a, s.n, COLS) * a.c.heads * span_of(a, s, s.p0, s.p0 + s.n - 1).pages;
 }
 
-// units of a workgroup's run, computed by every wavefront
-__device__ __forceinline__ int64_t run_length(const AttnArgs &a) {
+// The run of workgroup `w`: how many units a run has, and the sequence and place of its first one.  Every wavefront computes it.
+// Up to 64 sequences are a lane each, and one prefix sum gives both.
+__device__ __forceinline__ bool find_run(const AttnArgs &a, int64_t w, int64_t &run, int &seq, int64_t &inside) {
   const int lane = threadIdx.x & 63;
+  const auto run_of = [&](int64_t total) {
+    const int64_t even = (total + gridDim.x - 1) / gridDim.x;
+    return even > a.least ? even : a.least;
+  };
+  if (a.c.n_seqs <= 64) {
+    const int64_t units = lane < a.c.n_seqs ? units_of(a, lane) : 0;
+    if (!__any(units >= 1 << 24)) {  // 32 bits hold the sums
+      const int u = (int)units;
+      int sum = u;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(sum, d, 64);
+        if (lane >= d) sum += o;
+      }
+      run = run_of(__builtin_amdgcn_readlane(sum, 63));
+      const int64_t first = w * run;
+      const unsigned long long past = __ballot(sum > first);
+      if (!past) return false;
+      seq = __ffsll(past) - 1;
+      inside = first - __builtin_amdgcn_readlane(sum - u, seq);
+      return true;
+    }
+  }
   int64_t total = 0;
   for (int b = lane; b < a.c.n_seqs; b += 64) total += units_of(a, b);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d, 64);
-  const int64_t even = (total + gridDim.x - 1) / gridDim.x;
-  return even > a.least ? even : a.least;
+  run = run_of(total);
+  return find_piece(a.c.n_seqs, w * run, [&](int i) { return units_of(a, i); }, seq, inside);
 }
 
 template <typename T, int HD> struct Columns {
@@ -57,35 +81,46 @@ template <typename T, int HD> struct Columns {
   Sight sight;   // of this lane's column
 };
 
-template <typename T, int HD>
-__device__ __forceinline__ void load_columns(const AttnArgs &a, const Seq &s, int head, const Block &b, Columns<T, HD> &k) {
-  typedef Columns<T, HD> C;
-  const int lane = threadIdx.x & 63, g = lane >> 4;
-  const int c = b.col0 + (lane & 15), token = (int)((uint32_t)c / (uint32_t)a.rep);
-  const bool valid = (lane & 15) < b.cols;
-  float x[C::PARTS][8];
-  float amax = 0.0f;
-  if (valid) {
+// the elements of a lane's column as they are, on their way
+template <typename T, int HD> struct RawColumns {
+  static constexpr int WORDS = sizeof(T) / 2;  // 16-byte words of eight elements
+  u32x4 x[HD / 32][WORDS];
+  __device__ __forceinline__ RawColumns(const AttnArgs &a, const Seq &s, int head, const Block &b) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int c = b.col0 + (lane & 15), token = (int)((uint32_t)c / (uint32_t)a.rep);
     const T *q = (const T *)a.q + (int64_t)(s.row + token) * a.ldq + (int64_t)(head * a.rep + (c - token * a.rep)) * a.hsq;
 #pragma unroll
-    for (int m = 0; m < C::PARTS; ++m) load8<T>(q + (m >> 1) * 64 + g * 16 + (m & 1) * 8, x[m]);
-  } else {
+    for (int m = 0; m < HD / 32; ++m)
 #pragma unroll
-    for (int m = 0; m < C::PARTS; ++m)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[m][i] = 0.0f;
+      for (int i = 0; i < WORDS; ++i) {
+        x[m][i] = u32x4{0, 0, 0, 0};
+        if ((lane & 15) < b.cols) x[m][i] = reinterpret_cast<const u32x4 *>(q + (m >> 1) * 64 + g * 16 + (m & 1) * 8)[i];
+      }
   }
+};
+
+template <typename T, int HD>
+__device__ __forceinline__ void make_columns(const AttnArgs &a, const Seq &s, const Block &b, const RawColumns<T, HD> &raw, Columns<T, HD> &k) {
+  typedef Columns<T, HD> C;
+  const int lane = threadIdx.x & 63;
+  float x[C::PARTS][8];
+  float amax = 0.0f;
 #pragma unroll
   for (int m = 0; m < C::PARTS; ++m)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(x[m][i]));
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (C::SPLIT) x[m][i] = __uint_as_float(raw.x[m][i >> 2][i & 3]);
+      else x[m][i] = (float)__builtin_bit_cast(typename Vec8<T>::type, raw.x[m][0])[i];
+      amax = fmaxf(amax, fabsf(x[m][i]));
+    }
   amax = fmaxf(amax, __shfl_xor(amax, 16, 64));
   amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
   int e = (int)(__float_as_uint(amax) >> 23) - 127 - 8;  // largest element to [2^8, 2^9)
   e = e < -118 ? -118 : e;
   const float down = __uint_as_float((uint32_t)(127 - e) << 23);
   k.factor = ldexpf(a.scale, e);
-  k.sight = valid ? sight_of(a, s, s.p0 + token) : Sight{-1, -1};
+  const int token = (int)((uint32_t)(b.col0 + (lane & 15)) / (uint32_t)a.rep);
+  k.sight = (lane & 15) < b.cols ? sight_of(a, s, s.p0 + token) : Sight{-1, -1};
 #pragma unroll
   for (int m = 0; m < C::PARTS; ++m) {
 #pragma unroll
@@ -95,6 +130,24 @@ __device__ __forceinline__ void load_columns(const AttnArgs &a, const Seq &s, in
   }
 }
 
+// the codes of a page as a lane takes them
+template <int HD> struct PageCodes {
+  u32x4 k[4][HD / 64], v[HD / 16];
+  f32x2 scales;
+  __device__ __forceinline__ void load(const AttnArgs &a, int page, int head) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+    const uint8_t *kc = codes_of(a.c, page, head, 0), *vc = codes_of(a.c, page, head, 1);
+    scales = *reinterpret_cast<const f32x2 *>(scale_of(a.c, page, head, 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < HD / 64; ++j)  // row n of tile i is token 16 (n / 4) + 4 i + n % 4
+        k[i][j] = *reinterpret_cast<const u32x4 *>(kc + ((n >> 2) * 16 + i * 4 + (n & 3)) * HD + j * 64 + g * 16);
+#pragma unroll
+    for (int t = 0; t < HD / 16; ++t) v[t] = *reinterpret_cast<const u32x4 *>(vc + (t * 16 + n) * PAGE + g * 16);
+  }
+};
+
 // one wavefront's running result of 16 columns: lane (column n, group g) holds channels 16 t + 4 g + r
 template <int HD> struct State {
   f32x4 acc[HD / 16];
@@ -102,21 +155,10 @@ template <int HD> struct State {
 };
 
 template <typename T, int HD>
-__device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD> &k, State<HD> &st, int page, int head,
-                                          int t0, bool whole) {
+__device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD> &k, State<HD> &st, PageCodes<HD> &p, int t0, bool whole) {
   typedef Columns<T, HD> C;
-  const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
-  const uint8_t *kc = codes_of(a.c, page, head, 0), *vc = codes_of(a.c, page, head, 1);
-  const f32x2 scales = *reinterpret_cast<const f32x2 *>(scale_of(a.c, page, head, 0));
-  u32x4 kw[4][HD / 64], vw[HD / 16];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < HD / 64; ++j)  // row n of tile i is token 16 (n / 4) + 4 i + n % 4
-      kw[i][j] = *reinterpret_cast<const u32x4 *>(kc + ((n >> 2) * 16 + i * 4 + (n & 3)) * HD + j * 64 + g * 16);
-#pragma unroll
-  for (int t = 0; t < HD / 16; ++t) vw[t] = *reinterpret_cast<const u32x4 *>(vc + (t * 16 + n) * PAGE + g * 16);
-
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  const f32x2 scales = p.scales;
   const float factor = k.factor * scales[0];
   float s[16];
 #pragma unroll
@@ -124,7 +166,7 @@ __device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD
     f32x4 d = {0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < HD / 64; ++j) {
-      const f16x8 x = widen8(kw[i][j][0], kw[i][j][1]), y = widen8(kw[i][j][2], kw[i][j][3]);
+      const f16x8 x = widen8(p.k[i][j][0], p.k[i][j][1]), y = widen8(p.k[i][j][2], p.k[i][j][3]);
       if constexpr (C::SPLIT) {
         d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, k.lo[2 * j], d, 0, 0, 0);
         d = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, k.lo[2 * j + 1], d, 0, 0, 0);
@@ -135,12 +177,13 @@ __device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD
 #pragma unroll
     for (int r = 0; r < 4; ++r) s[4 * i + r] = d[r] * factor;
   }
-  bool visible[16];
+  uint32_t seen = 0;
   if (!whole) {
+    seen = seen_bits(a, k.sight, t0 + g * 16);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      visible[i] = sees(a, k.sight, t0 + g * 16 + i);
-      s[i] = visible[i] ? s[i] : -INFINITY;
+      const uint32_t m = spread_bit(seen, i);
+      s[i] = __uint_as_float((__float_as_uint(s[i]) & m) | (0xff800000u & ~m));  // hidden: -infinity
     }
   }
   float top = st.m;
@@ -180,25 +223,25 @@ __device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD
 #pragma unroll
     for (int t = 0; t < HD / 16; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= nan_bytes(vw[t][i]);
+      for (int i = 0; i < 4; ++i) bad |= nan_bytes(p.v[t][i]);
     bad = __ballot(bad != 0) != 0;
   }
   if (bad) {
-    f16x8 sees[2];
+    u32x4 ones[2];  // fp16 ones of the tokens that are seen
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sees[i >> 3][i & 7] = visible[i] ? (_Float16)1.0f : (_Float16)0.0f;
+    for (int i = 0; i < 8; ++i) ones[i >> 2][i & 3] = (spread_bit(seen, 2 * i) & 0x3c00u) | (spread_bit(seen, 2 * i + 1) & 0x3c000000u);
 #pragma unroll
     for (int t = 0; t < HD / 16; ++t) {
       u32x4 mark;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t b = nan_bytes(vw[t][i]) >> 7;  // 1 in the place of a NaN
+        const uint32_t b = nan_bytes(p.v[t][i]) >> 7;  // 1 in the place of a NaN
         mark[i] = b * 0x38u;                          // the code of 1.0
-        vw[t][i] &= ~(b * 0xffu);
+        p.v[t][i] &= ~(b * 0xffu);
       }
       f32x4 d = {0, 0, 0, 0};
-      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(mark[0], mark[1]), sees[0], d, 0, 0, 0);
-      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(mark[2], mark[3]), sees[1], d, 0, 0, 0);
+      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(mark[0], mark[1]), __builtin_bit_cast(f16x8, ones[0]), d, 0, 0, 0);
+      d = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(mark[2], mark[3]), __builtin_bit_cast(f16x8, ones[1]), d, 0, 0, 0);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         if (d[r] > 0.0f) st.acc[t][r] = __uint_as_float(0x7fc00000u);
@@ -206,7 +249,7 @@ __device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD
   }
 #pragma unroll
   for (int t = 0; t < HD / 16; ++t) {
-    const f16x8 x = widen8(vw[t][0], vw[t][1]), y = widen8(vw[t][2], vw[t][3]);
+    const f16x8 x = widen8(p.v[t][0], p.v[t][1]), y = widen8(p.v[t][2], p.v[t][3]);
     f32x4 d = st.acc[t] * fix;
     if constexpr (C::SPLIT) {
       d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, lo[0], d, 0, 0, 0);
@@ -223,11 +266,12 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_ker
   __shared__ float sh_acc[WAVES][COLS][HD + 4];
   __shared__ float sh_m[WAVES][COLS], sh_l[WAVES][COLS];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, n = lane & 15;
-  const int64_t run = run_length(a), w = blockIdx.x;
+  const int64_t w = blockIdx.x;
   int b;
-  int64_t inside;
+  int64_t run, inside;
   if (threadIdx.x == 0) a.header[w * 8 + H_PARTS] = 0;
-  if (!find_piece(a.c.n_seqs, w * run, [&](int i) { return units_of(a, i); }, b, inside)) return;
+  if (!find_run(a, w, run, b, inside)) return;
+  run = uniform(run);
   b = __builtin_amdgcn_readfirstlane(b);
   inside = uniform(inside);
   int64_t left = run;
@@ -244,20 +288,43 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_ker
       const Block k = block_of(a, s, (int)(item - (int64_t)head * blocks) * COLS, COLS);
       const int end = (int)min((int64_t)span.pages, x + left);
       left -= end - x;
+      // This wavefront's pages are x + wave + WAVES t, t < count.  A lane reads the table for one of them, 64 at a time.
+      const int mine = x + wave, count = end > mine ? (end - mine + WAVES - 1) / WAVES : 0;
+      const auto first_token = [&](int t) { return span.entry(mine + WAVES * t) * PAGE; };
+      const auto read_ids = [&](int t) {
+        const int at = t + lane;
+        return at < count && !none_sees(a, s, k, first_token(at)) ? page_of(a.c, b, span.entry(mine + WAVES * at)) : -1;
+      };
+      int ids = read_ids(0);
+      const RawColumns<T, HD> raw(a, s, head, k);
       Columns<T, HD> c;
-      load_columns<T, HD>(a, s, head, k, c);
       State<HD> st;
 #pragma unroll
       for (int t = 0; t < HD / 16; ++t) st.acc[t] = f32x4{0, 0, 0, 0};
       st.m = NEG;
       st.l = 0.0f;
       st.unit = 1.0f;
-      for (int i = x + wave; i < end; i += WAVES) {
-        const int entry = span.entry(i), t0 = entry * PAGE;
-        if (none_sees(a, s, k, t0)) continue;
-        const int page = __builtin_amdgcn_readfirstlane(page_of(a.c, b, entry));
-        if (page < 0) continue;
-        take_page<T, HD>(a, c, st, page, head, t0, all_see(a, s, k, t0));
+      const auto id_at = [&](int t) {
+        if (t >= count) return -1;
+        if (t && (t & 63) == 0) ids = read_ids(t);
+        return __builtin_amdgcn_readlane(ids, t & 63);
+      };
+      // While a page is worked on the next one's codes are on their way, where registers hold two.
+      constexpr bool TWO = HD == 64;
+      PageCodes<HD> even, odd;
+      int page = id_at(0);
+      if (page >= 0) even.load(a, page, head);
+      make_columns<T, HD>(a, s, k, raw, c);
+      const auto step = [&](int t, PageCodes<HD> &here, PageCodes<HD> &ahead) {
+        const int t0 = first_token(t), now = page;
+        page = id_at(t + 1);
+        if (TWO && page >= 0) ahead.load(a, page, head);
+        if (now >= 0) take_page<T, HD>(a, c, st, here, t0, all_see(a, s, k, t0));
+        if (!TWO && page >= 0) here.load(a, page, head);
+      };
+      for (int t = 0; t < count; t += TWO ? 2 : 1) {
+        step(t, even, odd);
+        if (TWO && t + 1 < count) step(t + 1, odd, even);
       }
       // the wavefronts' results together
       st.l += __shfl_xor(st.l, 16, 64);
@@ -321,36 +388,71 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_ker
   }
 }
 
-// Joins the parts of the item that begins in run blockIdx.x and goes on: a wavefront per column.  The first part lies at
-// H_FIRST, the others at the beginnings of the following runs.
+// Joins the parts of the item that begins in run blockIdx.x and goes on, column by column: the first part lies at H_FIRST, the
+// others at the beginnings of the following runs.  Maxima and sums of all parts are fetched together, then each wavefront adds up
+// a quarter of the parts, the first few of them requested along with the maxima.
+constexpr int MOST_GROUPS = 1024;
 template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void cache8_join_kernel(const AttnArgs a) {
-  const int64_t w = blockIdx.x;
-  const int64_t *hd = a.header + w * 8;
-  const int64_t parts = hd[H_PARTS];
-  const int c = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (!parts || c >= hd[H_COLS]) return;
-  const auto part = [&](int64_t i) { return a.part + ((i ? 2 * (w + i) : hd[H_FIRST]) * WIDTH + c) * (HD + 2); };
-  float top = NEG;
-  for (int64_t i = lane; i < parts; i += 64) top = fmaxf(top, part(i)[HD]);
+  __shared__ float sh_w[MOST_GROUPS + 1], sh_red[8];
+  __shared__ float sh_o[4][HD];
+  const int w = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int64_t *hd = a.header + (int64_t)w * 8;
+  const int parts = (int)hd[H_PARTS], cols = (int)hd[H_COLS], slot0 = (int)hd[H_FIRST];
+  if (!parts) return;
+  typedef float Out __attribute__((ext_vector_type(HD / 64)));  // a lane's channels
+  for (int c = blockIdx.y; c < cols; c += gridDim.y) {
+    const auto part = [&](int i) { return a.part + ((int64_t)(i ? 2 * (w + i) : slot0) * WIDTH + c) * (HD + 2); };
+    const auto values = [&](int i) {
+      const float *p = part(i) + lane * (HD / 64);
+      Out o;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
-  float sum = 0.0f, o[HD / 64];
+      for (int j = 0; j < HD / 64; ++j) o[j] = p[j];
+      return o;
+    };
+    constexpr int EARLY = 4;
+    Out early[EARLY];
 #pragma unroll
-  for (int j = 0; j < HD / 64; ++j) o[j] = 0.0f;
+    for (int e = 0; e < EARLY; ++e) early[e] = wave + 4 * e < parts ? values(wave + 4 * e) : Out{};
+    float top = NEG;
+    for (int i = t; i < parts; i += 256) {
+      const float m = part(i)[HD];
+      sh_w[i] = m;
+      top = fmaxf(top, m);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+    if (lane == 0) sh_red[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(sh_red[0], sh_red[1]), fmaxf(sh_red[2], sh_red[3]));
+    float sum = 0.0f;
+    for (int i = t; i < parts; i += 256) {
+      const float x = __builtin_amdgcn_exp2f(sh_w[i] - top);
+      sh_w[i] = x;
+      sum += x * part(i)[HD + 1];
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
+    if (lane == 0) sh_red[4 + wave] = sum;
+    __syncthreads();
+    Out o = {};
+#pragma unroll
+    for (int e = 0; e < EARLY; ++e)
+      if (wave + 4 * e < parts) o += sh_w[wave + 4 * e] * early[e];
 #pragma unroll 8
-  for (int64_t i = 0; i < parts; ++i) {
-    const float *p = part(i);
-    const float x = __builtin_amdgcn_exp2f(p[HD] - top);
-    sum += x * p[HD + 1];
+    for (int i = wave + 4 * EARLY; i < parts; i += 4) o += sh_w[i] * values(i);
 #pragma unroll
-    for (int j = 0; j < HD / 64; ++j) o[j] += x * p[j * 64 + lane];
+    for (int j = 0; j < HD / 64; ++j) sh_o[wave][lane * (HD / 64) + j] = o[j];
+    __syncthreads();
+    if (t < HD) {
+      sum = (sh_red[4] + sh_red[5]) + (sh_red[6] + sh_red[7]);
+      const float x = (sh_o[0][t] + sh_o[1][t]) + (sh_o[2][t] + sh_o[3][t]);
+      const uint32_t col = (uint32_t)hd[H_COL0] + c, token = col / (uint32_t)a.rep;
+      const int64_t h = hd[H_HEAD] * a.rep + (col - token * a.rep);
+      T *out = (T *)a.out + (hd[H_ROW] + token) * a.ldo + h * a.hso;
+      out[t] = (T)(sum != 0.0f ? x * (1.0f / sum) : 0.0f);
+    }
+    __syncthreads();
   }
-  const uint32_t col = (uint32_t)hd[H_COL0] + c, token = col / (uint32_t)a.rep;
-  const int64_t h = hd[H_HEAD] * a.rep + (col - token * a.rep);
-  T *out = (T *)a.out + (hd[H_ROW] + token) * a.ldo + h * a.hso;
-  const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-  for (int j = 0; j < HD / 64; ++j) out[j * 64 + lane] = (T)(sum != 0.0f ? o[j] * over : 0.0f);
 }
 
 int attn_cus() {
@@ -373,7 +475,7 @@ Plan plan_of(int cus, int32_t dtype, int64_t rows, int n_seqs, int heads, int re
   const int64_t seqs = rows < n_seqs ? rows : n_seqs, cols = rows * rep;
   p.many = dtype != RVQ_F32 && cols > 2 * COLS * seqs;
   const int per_cu = p.many && hd == 256 ? 1 : 2;
-  p.groups = per_cu * cus;
+  p.groups = per_cu * cus < MOST_GROUPS ? per_cu * cus : MOST_GROUPS;
   const int64_t items = cols / MANY * heads;  // at least
   p.whole = p.many && items >= 2 * p.groups && (cols / MANY + seqs) * heads <= INT32_MAX;
   if (p.whole) p.groups = (cols / MANY + seqs) * heads;
@@ -385,13 +487,13 @@ template <typename T, int HD> void launch_attn(const AttnArgs &a, const Plan &p,
   if constexpr (!std::is_same<T, float>::value) {
     if (p.many) {
       rvq_launch_cache8_chunk(a, std::is_same<T, _Float16>::value, p.groups, p.whole, s);
-      if (!p.whole) hipLaunchKernelGGL((cache8_join_kernel<T, HD, MANY>), dim3(grid.x, MANY / 4), dim3(256), 0, s, a);
+      if (!p.whole) hipLaunchKernelGGL((cache8_join_kernel<T, HD, MANY>), dim3(grid.x, 16), dim3(256), 0, s, a);
       return;
     }
   }
   hipLaunchKernelGGL((cache8_attn_kernel<T, HD>), grid, dim3(64 * WAVES), 0, s, a);
   const int64_t cols = a.c.rows * a.rep < COLS ? a.c.rows * a.rep : COLS;
-  hipLaunchKernelGGL((cache8_join_kernel<T, HD, COLS>), dim3(grid.x, (unsigned)(cols + 3) / 4), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((cache8_join_kernel<T, HD, COLS>), dim3(grid.x, (unsigned)cols), dim3(256), 0, s, a);
 }
 template <typename T> void launch_attn_hd(const AttnArgs &a, const Plan &p, hipStream_t s) {
   if (a.c.hd == 64) launch_attn<T, 64>(a, p, s);

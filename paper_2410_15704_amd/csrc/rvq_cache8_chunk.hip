@@ -19,29 +19,33 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
+template <typename T> struct Vec4 {
+  typedef T type __attribute__((ext_vector_type(4)));
+};
+
 constexpr float CHUNK_BITS = 8.0f;  // weights are held as 2^8 2^(s - m)
 
 // The blocks of all sequences, 256 per trip, one per thread: visit(sequence, block, pages), pages = 0 for none, is called by all
 // threads together until it returns true in all of them.  A block's sequence is found by bisection of the sequences' prefix sums.
 struct Shared {
-  int64_t before[257], wave[4];
-  int found[3];
-  int64_t rest;
+  int before[257], wave[4], found[3];
+  int64_t wave64[4], rest;
   int pages_like[512];
   int flags[WAVES];
 };
-__device__ __forceinline__ int64_t scan256(int64_t x, int64_t *wave, int64_t &total) {
+// inclusive prefix sums over the workgroup's threads
+template <typename N> __device__ __forceinline__ N scan256(N x, N *wave, N &total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int64_t sum = x;
+  N sum = x;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int64_t o = __shfl_up(sum, d, 64);
+    const N o = __shfl_up(sum, d, 64);
     if (lane >= d) sum += o;
   }
   __syncthreads();
   if (lane == 63) wave[w] = sum;
   __syncthreads();
-  int64_t add = 0;
+  N add = 0;
   total = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -50,28 +54,39 @@ __device__ __forceinline__ int64_t scan256(int64_t x, int64_t *wave, int64_t &to
   }
   return sum + add;
 }
-template <typename Visit> __device__ __forceinline__ void walk(const AttnArgs &a, Shared &sh, Visit visit) {
+// the 256 sequences from b0 on: their blocks, and prefix sums in `before`
+__device__ __forceinline__ int count_blocks(const AttnArgs &a, Shared &sh, int b0) {
   const int t = threadIdx.x;
-  for (int b0 = 0; b0 < a.c.n_seqs; b0 += 256) {
-    int64_t blocks;
-    const int64_t upto = scan256(b0 + t < a.c.n_seqs ? blocks_of(a, rows_of(a.c, b0 + t).n, MANY) : 0, sh.wave, blocks);
-    sh.before[t + 1] = upto;
-    if (t == 0) sh.before[0] = 0;
-    __syncthreads();
-    for (int64_t k0 = 0; k0 < blocks; k0 += 256) {
-      const int64_t k = k0 + t;
-      int s = 0, j = 0, pages = 0;
-      if (k < blocks) {
+  int blocks;
+  const int upto = scan256(b0 + t < a.c.n_seqs ? blocks_of(a, rows_of(a.c, b0 + t).n, MANY) : 0, sh.wave, blocks);
+  sh.before[t + 1] = upto;
+  if (t == 0) sh.before[0] = 0;
+  __syncthreads();
+  return blocks;
+}
+// block k of them: its sequence, its place there and its pages (0: there is no such block)
+struct Place {
+  int b, j, pages;
+};
+__device__ __forceinline__ Place place_of(const AttnArgs &a, const Shared &sh, int b0, int k, int blocks) {
+  Place p = {0, 0, 0};
+  if (k >= blocks) return p;
+  int s = 0;
 #pragma unroll
-        for (int d = 128; d; d /= 2)
-          if (sh.before[s + d] <= k) s += d;
-        j = (int)(k - sh.before[s]);
-        const Seq q = seq_of(a, b0 + s);
-        const Block x = block_of(a, q, j * MANY, MANY);
-        pages = span_of(a, q, x.first, x.last).pages;
-      }
-      if (visit(b0 + s, j, pages)) return;
-    }
+  for (int d = 128; d; d /= 2)
+    if (sh.before[s + d] <= k) s += d;
+  p.b = b0 + s;
+  p.j = k - sh.before[s];
+  const Seq q = seq_of(a, p.b);
+  const Block x = block_of(a, q, p.j * MANY, MANY);
+  p.pages = span_of(a, q, x.first, x.last).pages;
+  return p;
+}
+template <typename Visit> __device__ __forceinline__ void walk(const AttnArgs &a, Shared &sh, Visit visit) {
+  for (int b0 = 0; b0 < a.c.n_seqs; b0 += 256) {
+    const int blocks = count_blocks(a, sh, b0);
+    for (int k0 = 0; k0 < blocks; k0 += 256)
+      if (visit(place_of(a, sh, b0, k0 + (int)threadIdx.x, blocks))) return;
     __syncthreads();
   }
 }
@@ -79,11 +94,11 @@ template <typename Visit> __device__ __forceinline__ void walk(const AttnArgs &a
 // pages of all items
 __device__ __forceinline__ int64_t all_units(const AttnArgs &a, Shared &sh) {
   int64_t mine = 0, total;
-  walk(a, sh, [&](int, int, int pages) {
-    mine += (int64_t)pages * a.c.heads;
+  walk(a, sh, [&](const Place &p) {
+    mine += (int64_t)p.pages * a.c.heads;
     return false;
   });
-  (void)scan256(mine, sh.wave, total);
+  (void)scan256(mine, sh.wave64, total);
   return total;
 }
 
@@ -91,13 +106,13 @@ __device__ __forceinline__ int64_t all_units(const AttnArgs &a, Shared &sh) {
 __device__ __forceinline__ void find_unit(const AttnArgs &a, Shared &sh, int64_t target) {
   int64_t base = 0;
   if (threadIdx.x == 0) sh.found[0] = -1;
-  walk(a, sh, [&](int b, int j, int pages) {
-    const int64_t units = (int64_t)pages * a.c.heads;
+  walk(a, sh, [&](const Place &p) {
+    const int64_t units = (int64_t)p.pages * a.c.heads;
     int64_t total;
-    const int64_t at = base + scan256(units, sh.wave, total) - units;
+    const int64_t at = base + scan256(units, sh.wave64, total) - units;
     if (at <= target && target < at + units) {
-      sh.found[0] = b;
-      sh.found[1] = j;
+      sh.found[0] = p.b;
+      sh.found[1] = p.j;
       sh.rest = target - at;
     }
     __syncthreads();
@@ -112,39 +127,45 @@ __device__ __forceinline__ int class_of(int pages) {
   return 511 - (e * 16 + (int)(((int64_t)pages << 4) >> e) - 16);
 }
 // the block of that rank: found[0], found[1]; found[0] < 0: there are not so many
-__device__ __forceinline__ void find_rank(const AttnArgs &a, Shared &sh, int64_t rank) {
+__device__ __forceinline__ void find_rank(const AttnArgs &a, Shared &sh, int rank) {
   const int t = threadIdx.x;
   sh.pages_like[t] = sh.pages_like[t + 256] = 0;
   if (t == 0) sh.found[0] = sh.found[2] = -1;
-  walk(a, sh, [&](int, int, int pages) {  // (barriers of the walk come before the first count)
-    if (pages) atomicAdd(&sh.pages_like[class_of(pages)], 1);
+  Place last = {0, 0, 0};
+  int trips = 0;
+  walk(a, sh, [&](const Place &p) {  // (barriers of the walk come before the first count)
+    if (p.pages) atomicAdd(&sh.pages_like[class_of(p.pages)], 1);
+    last = p;
+    ++trips;
     return false;
   });
   __syncthreads();
-  const int two = sh.pages_like[2 * t] + sh.pages_like[2 * t + 1];
-  int64_t total;
-  const int64_t at = scan256(two, sh.wave, total) - two;
+  const int one = sh.pages_like[2 * t], two = one + sh.pages_like[2 * t + 1];
+  int total;
+  const int at = scan256(two, sh.wave, total) - two;
   if (at <= rank && rank < at + two) {
-    const bool second = rank >= at + sh.pages_like[2 * t];
+    const bool second = rank >= at + one;
     sh.found[2] = 2 * t + second;
-    sh.rest = rank - at - (second ? sh.pages_like[2 * t] : 0);
+    sh.before[0] = rank - at - (second ? one : 0);
   }
   __syncthreads();
-  const int cls = sh.found[2];
+  const int cls = sh.found[2], place = sh.before[0];
   if (cls < 0) return;
-  const int64_t place = sh.rest;
-  int64_t base = 0;
-  walk(a, sh, [&](int b, int j, int pages) {
-    const int hit = pages && class_of(pages) == cls;
-    const int64_t before = base + scan256(hit, sh.wave, total) - hit;
+  __syncthreads();  // `before` is written again
+  int base = 0;
+  const auto look = [&](const Place &p) {
+    const int hit = p.pages && class_of(p.pages) == cls;
+    const int before = base + scan256(hit, sh.wave, total) - hit;
     if (hit && before == place) {
-      sh.found[0] = b;
-      sh.found[1] = j;
+      sh.found[0] = p.b;
+      sh.found[1] = p.j;
     }
     __syncthreads();
     base += total;
     return sh.found[0] >= 0;
-  });
+  };
+  if (trips == 1) look(last);  // every thread still holds its block
+  else walk(a, sh, look);
 }
 
 // A query as e4m3 terms for the products with the keys' codes as they are: 4 bits each, the next one 2^-4 of the last, so
@@ -260,14 +281,6 @@ __device__ __forceinline__ Range range_of(const AttnArgs &a, const Seq &s, const
   return r;
 }
 
-// bit i: this lane's column sees token t0 + i, i < 32
-__device__ __forceinline__ uint32_t ones(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
-__device__ __forceinline__ uint32_t seen_bits(const AttnArgs &a, const Sight &x, int t0) {
-  return ones(x.to - t0 + 1) & (~ones(x.hidden - t0 + 1) | ones(a.sinks - t0));
-}
-// all bits of the result are bit i of x
-__device__ __forceinline__ uint32_t spread_bit(uint32_t x, int i) { return (uint32_t)((int)(x << (31 - i)) >> 31); }
-
 // One page for this wavefront's columns.  `whole`: every column sees every token; values' codes hold no NaN otherwise.
 template <typename T, int HD>
 __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> &k, const uint8_t *codes, float kscale, float vscale,
@@ -290,16 +303,19 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
         s[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, k.q[c][t], s[i], 0, 0, 0, 127, 0, 127 - 4 * t);
     }
   }
-  // the values' codes are on their way while the weights are made
-  u32x4 v[HD / 32][2];
+  // the values' codes are on their way while the weights are made, where registers allow it
+  constexpr bool EARLY = HD <= 128;
+  u32x4 v[EARLY ? HD / 32 : 1][2];
+  const auto load_values = [&](int c, u32x4(&to)[2]) {
+    const int row = c * 32 + n;
 #pragma unroll
-  for (int c = 0; c < HD / 32; ++c)
+    for (int i = 0; i < 2; ++i) to[i] = *reinterpret_cast<const u32x4 *>(vc + row * PAGE + value_piece(row, 2 * h + i) * 16);
+  };
+  if constexpr (EARLY) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row = c * 32 + n;
-      v[c][i] = *reinterpret_cast<const u32x4 *>(vc + row * PAGE + value_piece(row, 2 * h + i) * 16);
-    }
-  __builtin_amdgcn_sched_barrier(0);
+    for (int c = 0; c < HD / 32; ++c) load_values(c, v[c]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
   if (!whole) {
     const uint32_t seen = seen_bits(a, k.sight, t0 + h * 32);
 #pragma unroll
@@ -359,10 +375,13 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
   }
   k.l += sum * count;
 #pragma unroll
-  for (int c = 0; c < HD / 32; ++c)
+  for (int c = 0; c < HD / 32; ++c) {
+    u32x4(&x)[2] = v[EARLY ? c : 0];
+    if constexpr (!EARLY) load_values(c, x);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      k.acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(v[c][i >> 1][(i & 1) * 2], v[c][i >> 1][(i & 1) * 2 + 1]), w[i], k.acc[c], 0, 0, 0);
+      k.acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(x[i >> 1][(i & 1) * 2], x[i >> 1][(i & 1) * 2 + 1]), w[i], k.acc[c], 0, 0, 0);
+  }
 }
 
 // A NaN among the values' codes of a slot that some column does not see must not meet its weight of 0.  For pages that not
@@ -426,7 +445,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
   int b, head, j, x = 0;
   int64_t left, run = 1;
   if (whole_items) {
-    find_rank(a, sh, w / a.c.heads);
+    find_rank(a, sh, (int)(w / a.c.heads));
     if (sh.found[0] < 0) return;
     b = sh.found[0];
     j = sh.found[1];
@@ -515,9 +534,12 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
 #pragma unroll
         for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
+          for (int q = 0; q < 4; ++q) {
+            typename Vec4<T>::type o;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) out[t * 32 + q * 8 + r] = (T)(some ? c.acc[t][q * 4 + r] * over : 0.0f);
+            for (int r = 0; r < 4; ++r) o[r] = (T)(some ? c.acc[t][q * 4 + r] * over : 0.0f);
+            *reinterpret_cast<typename Vec4<T>::type *>(out + t * 32 + q * 8) = o;
+          }
       } else {
         float *p = a.part + ((2 * w + (at_start ? 0 : 1)) * MANY + col) * (HD + 2);
 #pragma unroll
