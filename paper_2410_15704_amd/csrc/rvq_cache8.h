@@ -46,16 +46,16 @@ __device__ __forceinline__ float *scale_of(const CacheView &c, int64_t page, int
 // Finds the piece `at` of the sequences' pieces in order: sequence and place inside it.  Every wavefront does
 // it for itself, 64 sequences per trip: a prefix sum over the lanes and the first lane that passes `at`.
 // count(b) is called with b < n_seqs.  false: there are not so many.
-template <typename Count>
-__device__ __forceinline__ bool find_piece(int n_seqs, int64_t at, Count count, int &seq, int64_t &inside) {
+template <typename N, typename Count>
+__device__ __forceinline__ bool find_piece(int n_seqs, N at, Count count, int &seq, N &inside) {
   const int lane = threadIdx.x & 63;
-  int64_t before = 0;
+  N before = 0;
   for (int b0 = 0; b0 < n_seqs; b0 += 64) {
     const int b = b0 + lane;
-    int64_t c = b < n_seqs ? count(b) : 0, sum = c;
+    N c = b < n_seqs ? count(b) : 0, sum = c;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-      const int64_t o = __shfl_up(sum, d, 64);
+      const N o = __shfl_up(sum, d, 64);
       if (lane >= d) sum += o;
     }
     const unsigned long long past = __ballot(before + sum > at);

@@ -1,12 +1,14 @@
 // The paged cache of 8-bit codes: appending a step's tokens, and reading tokens back.
 //
 // Both are bound by memory: 2 or 4 bytes of a row element against one byte of code.  A workgroup takes one
-// page and kv head, keys or values: it holds every token of a scale, so the scale needs no second pass over
-// memory and no atomics, and results do not depend on any order.  The pages of the step are enumerated on the
-// device (find_piece), since only the device knows the lengths; the grid is an upper bound.
+// page and kv head, half of its threads the keys and half the values: it holds every token of a scale, so the scale
+// needs no second pass over memory and no atomics, and results do not depend on any order.  The pages of the step are
+// enumerated on the device (find_piece), since only the device knows the lengths; the grid is an upper bound.
 //
 // Keys are stored by token, values by channel (the order in which attention feeds both to the matrix cores
-// without a transposition), so the values' tile is turned in LDS here, once per token instead of once per reading.
+// without a transposition).  A thread of the values takes four channels of 16 tokens: its reads and writes of rows are 8 or
+// 16 bytes, neighbours beside each other along the row, and of codes 16 bytes of a channel; what lies between is
+// a transposition of 4 x 4 bytes in registers (reading), or none (the conversion packs neighbouring tokens).
 #include "rvq_cache8.h"
 
 namespace {
@@ -31,13 +33,13 @@ struct Span {
 };
 
 template <bool READ> __device__ __forceinline__ bool find_span(const MoveArgs &a, Span &s) {
-  int64_t inside;
+  int inside;
   const auto first_position = [&](int b, int n) -> int64_t { return READ ? a.first[b] : (int64_t)a.c.lengths[b] - n; };
-  const auto count = [&](int b) -> int64_t {
+  const auto count = [&](int b) -> int {
     const SeqRows r = rows_of(a.c, b);
-    return r.n ? pages_spanned(first_position(b, r.n), r.n) : 0;
+    return r.n ? (int)pages_spanned(first_position(b, r.n), r.n) : 0;
   };
-  if (!find_piece(a.c.n_seqs, blockIdx.x, count, s.b, inside)) return false;
+  if (!find_piece<int>(a.c.n_seqs, blockIdx.x / a.c.heads, count, s.b, inside)) return false;
   const SeqRows r = rows_of(a.c, s.b);
   s.n = r.n;
   s.row = r.row;
@@ -50,180 +52,240 @@ template <bool READ> __device__ __forceinline__ bool find_span(const MoveArgs &a
   return true;
 }
 
+// Loads are made for every slot, of the nearest one that the step has, and what does not belong is dropped afterwards: a load
+// under a condition would be waited for before the next one.
+__device__ __forceinline__ int nearest(const Span &s, int slot) { return slot < s.lo ? s.lo : slot >= s.hi ? s.hi - 1 : slot; }
+
 // slot of a unit -> row of the step
 __device__ __forceinline__ int64_t row_of(const Span &s, int slot) { return s.row + (s.entry * PAGE + slot - s.p0); }
 
-// 16 codes rounded again to a larger scale
+// codes rounded again to a larger scale
 __device__ __forceinline__ uint32_t again4(uint32_t w, float ratio) {
   float v[4];
   decode4(w, v);
   return encode4_any(v[0] * ratio, v[1] * ratio, v[2] * ratio, v[3] * ratio);
 }
 
-template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(256) void cache8_append_kernel(const MoveArgs a) {
-  constexpr int UNITS = HD / 16, PER = PAGE * UNITS / 256, LDR = HD + 16;
-  __shared__ float wave_max[4];
-  __shared__ __align__(16) uint8_t tile[PAGE * LDR];
+// Keys: 16 channels (unit u) of the four tokens first + 16 j.  Values: channels ch0 .. ch0 + 3 of tokens first .. first + 15.
+template <int HD> struct Task {
+  bool values;
+  int first, u, ch0;
+  __device__ __forceinline__ Task() {
+    const int t = threadIdx.x % HD;
+    values = threadIdx.x >= HD;
+    u = t % (HD / 16);
+    ch0 = t % (HD / 4) * 4;
+    first = values ? t / (HD / 4) * 16 : t / (HD / 16);
+  }
+};
+template <typename T> struct Vec4 {
+  typedef T type __attribute__((ext_vector_type(4)));
+};
+
+template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) void cache8_append_kernel(const MoveArgs a) {
+  __shared__ float wave_max[2 * HD / 64];
   Span s;
   if (!find_span<false>(a, s) || s.page < 0) return;
-  const int head = blockIdx.y >> 1, values = blockIdx.y & 1;
-  const T *src = (const T *)(values ? a.v : a.k) + head * (values ? a.hsv : a.hsk);
-  const int64_t ld = values ? a.ldv : a.ldk;
-  const int rot = values ? 0 : a.rot;
-  float *scale_at = scale_of(a.c, s.page, head, values);
+  const int head = blockIdx.x % a.c.heads;
+  const Task<HD> task;
+  float *scale_at = scale_of(a.c, s.page, head, task.values);
   const float old = s.lo ? *scale_at : 0.0f;
+  uint8_t *codes = codes_of(a.c, s.page, head, task.values);
 
-  float x[PER][16];
+  float x[4][16];  // keys [token][channel], values [channel][token]
+  int c0 = 0, c1 = 0;
+  if (!task.values) {
+    unit_channels<LAYOUT>(task.u, a.rot, c0, c1);
+    const T *src = (const T *)a.k + head * a.hsk;
+    typename Raw8<T>::type va[4], vb[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const T *p = src + row_of(s, nearest(s, task.first + 16 * j)) * a.ldk;
+      va[j] = raw8<T>(p + c0);
+      vb[j] = raw8<T>(p + c1);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float p[8], q[8];
+      widen<T>(va[j], p);
+      widen<T>(vb[j], q);
+      if (16 * task.u < a.rot) {
+        const int64_t row = row_of(s, nearest(s, task.first + 16 * j));
+        float cs[8], sn[8];
+        load8<float>(a.cos + row * (a.rot / 2) + 8 * task.u, cs);
+        load8<float>(a.sin + row * (a.rot / 2) + 8 * task.u, sn);
+        rotate_unit<LAYOUT>(p, q, cs, sn);
+      }
+      const int slot = task.first + 16 * j;
+      const bool in = slot >= s.lo && slot < s.hi;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[j][i] = in ? p[i] : 0.0f;
+        x[j][8 + i] = in ? q[i] : 0.0f;
+      }
+    }
+  } else if (task.first < s.hi && task.first + 16 > s.lo) {
+    const T *src = (const T *)a.v + head * a.hsv + task.ch0;
+    typename Vec4<T>::type v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      v[i] = *reinterpret_cast<const typename Vec4<T>::type *>(src + row_of(s, nearest(s, task.first + i)) * a.ldv);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j][i] = task.first + i >= s.lo && task.first + i < s.hi ? (float)v[i][j] : 0.0f;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[j][i] = 0.0f;
+  }
   float amax = 0.0f;
 #pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int id = j * 256 + (int)threadIdx.x, slot = id / UNITS, u = id % UNITS;
-    if (slot < s.lo || slot >= s.hi) continue;
-    int c0, c1;
-    unit_channels<LAYOUT>(u, rot, c0, c1);
-    const int64_t row = row_of(s, slot);
-    const T *p = src + row * ld;
-    float va[8], vb[8];
-    load8<T>(p + c0, va);
-    load8<T>(p + c1, vb);
-    if (16 * u < rot) {
-      float cs[8], sn[8];
-      load8<float>(a.cos + row * (rot / 2) + 8 * u, cs);
-      load8<float>(a.sin + row * (rot / 2) + 8 * u, sn);
-      rotate_unit<LAYOUT>(va, vb, cs, sn);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[j][i] = va[i];
-      x[j][8 + i] = vb[i];
-    }
+  for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int i = 0; i < 16; ++i) amax = not_finite(x[j][i]) ? amax : fmaxf(amax, fabsf(x[j][i]));
-  }
 #pragma unroll
   for (int d = 32; d; d /= 2) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
   if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = amax;
   __syncthreads();  // also: every thread has read the old scale
-  amax = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+#pragma unroll
+  for (int w = 0; w < HD / 64; ++w) amax = fmaxf(amax, wave_max[(task.values ? HD / 64 : 0) + w]);
   float scale = code_scale(amax);
   scale = s.lo ? fmaxf(scale, old) : scale;
   const bool grown = s.lo && scale > old;
   const float inverse = 1.0f / scale, ratio = grown ? old * inverse : 1.0f;
-  if (threadIdx.x == 0) *scale_at = scale;
+  if (threadIdx.x % HD == 0) *scale_at = scale;
 
-  uint8_t *codes = codes_of(a.c, s.page, head, values);
+  u32x4 w[4];
 #pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int id = j * 256 + (int)threadIdx.x, slot = id / UNITS, u = id % UNITS;
-    if (slot < s.lo || slot >= s.hi) continue;
-    int c0, c1;
-    unit_channels<LAYOUT>(u, rot, c0, c1);
-    u32x2 w0, w1;
+  for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float *p = &x[j][4 * i], *q = &x[j][8 + 4 * i];
-      w0[i] = encode4_any(p[0] * inverse, p[1] * inverse, p[2] * inverse, p[3] * inverse);
-      w1[i] = encode4_any(q[0] * inverse, q[1] * inverse, q[2] * inverse, q[3] * inverse);
+    for (int i = 0; i < 4; ++i)
+      w[j][i] = encode4_any(x[j][4 * i] * inverse, x[j][4 * i + 1] * inverse, x[j][4 * i + 2] * inverse, x[j][4 * i + 3] * inverse);
+  if (!task.values) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int slot = task.first + 16 * j;
+      if (slot < s.lo || slot >= s.hi) continue;
+      *reinterpret_cast<u32x2 *>(codes + slot * HD + c0) = u32x2{w[j][0], w[j][1]};
+      *reinterpret_cast<u32x2 *>(codes + slot * HD + c1) = u32x2{w[j][2], w[j][3]};
     }
-    uint8_t *to = values ? tile + slot * LDR : codes + slot * HD;
-    *reinterpret_cast<u32x2 *>(to + c0) = w0;
-    *reinterpret_cast<u32x2 *>(to + c1) = w1;
-  }
-  if (!values) {
     if (grown)  // the page's earlier tokens
-      for (int at = threadIdx.x * 16; at < s.lo * HD; at += 256 * 16) {
-        u32x4 w = *reinterpret_cast<const u32x4 *>(codes + at);
+      for (int at = threadIdx.x * 16; at < s.lo * HD; at += HD * 16) {
+        u32x4 v = *reinterpret_cast<const u32x4 *>(codes + at);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = again4(w[i], ratio);
-        *reinterpret_cast<u32x4 *>(codes + at) = w;
+        for (int i = 0; i < 4; ++i) v[i] = again4(v[i], ratio);
+        *reinterpret_cast<u32x4 *>(codes + at) = v;
       }
     return;
   }
-  __syncthreads();
-  // a thread writes 16 slots of one channel: whole where they are all new, else what is new, or what is old and changes
-  for (int id = threadIdx.x; id < HD * 4; id += 256) {
-    const int c = id >> 2, s0 = (id & 3) * 16;
-    uint8_t *to = codes + c * PAGE + s0;
-    const bool any_new = s0 < s.hi && s0 + 16 > s.lo, any_old = s0 < s.lo;
-    if (!any_new && !(any_old && grown)) continue;
-    u32x4 w = {0, 0, 0, 0};
-    const bool all_new = s0 >= s.lo && s0 + 16 <= s.hi;
-    if (!all_new) w = *reinterpret_cast<const u32x4 *>(to);
+  // 16 slots of a channel: whole where they are all new; read and written again where old ones change; else the new bytes alone
+  const int from = s.lo - task.first, to = s.hi - task.first;
+  if (from <= 0 && to >= 16) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t was = w[i], more = grown ? again4(was, ratio) : was;
-      uint32_t put = 0;
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4 *>(codes + (task.ch0 + j) * PAGE + task.first) = w[j];
+  } else if (grown && from > 0) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int slot = s0 + 4 * i + j;
-        const uint32_t from = slot < s.lo ? more >> (8 * j) : slot < s.hi ? tile[slot * LDR + c] : was >> (8 * j);
-        put |= (from & 0xffu) << (8 * j);
+    for (int j = 0; j < 4; ++j) {
+      u32x4 *at = reinterpret_cast<u32x4 *>(codes + (task.ch0 + j) * PAGE + task.first);
+      u32x4 v = *at;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t more = again4(v[i], ratio);
+        uint32_t put = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int slot = 4 * i + b;
+          put |= (slot < from ? more : slot < to ? w[j][i] : v[i]) & (0xffu << (8 * b));
+        }
+        v[i] = put;
       }
-      w[i] = put;
+      *at = v;
     }
-    *reinterpret_cast<u32x4 *>(to) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i >= from && i < to)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) codes[(task.ch0 + j) * PAGE + task.first + i] = (uint8_t)(w[j][i >> 2] >> (8 * (i & 3)));
   }
 }
 
-template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(256) void cache8_read_kernel(const MoveArgs a) {
-  constexpr int UNITS = HD / 16, PER = PAGE * UNITS / 256, LDR = HD + 16;
-  __shared__ __align__(16) uint8_t tile[PAGE * LDR];
+template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) void cache8_read_kernel(const MoveArgs a) {
   Span s;
   if (!find_span<true>(a, s)) return;
-  const int head = blockIdx.y >> 1, values = blockIdx.y & 1;
-  T *dst = (T *)(values ? a.v : a.k);
+  const int head = blockIdx.x % a.c.heads;
+  const Task<HD> task;
+  T *dst = (T *)(task.values ? a.v : a.k);
   if (!dst) return;
-  dst += head * (values ? a.hsv : a.hsk);
-  const int64_t ld = values ? a.ldv : a.ldk;
-  const int rot = values ? 0 : a.rot;
+  dst += head * (task.values ? a.hsv : a.hsk);
   // slots that hold a token of the sequence
   const int64_t end = (int64_t)a.c.lengths[s.b] - s.entry * PAGE;
   const int held = s.page < 0 ? 0 : (int)(end < 0 ? 0 : end > PAGE ? PAGE : end);
-  const uint8_t *codes = s.page < 0 ? nullptr : codes_of(a.c, s.page, head, values);
-  const float scale = s.page < 0 ? 0.0f : *scale_of(a.c, s.page, head, values);
-  if (values && held) {
-    for (int id = threadIdx.x; id < HD * 4; id += 256) {
-      const int c = id >> 2, s0 = (id & 3) * 16;
-      if (s0 >= s.hi || s0 + 16 <= s.lo) continue;
-      const u32x4 w = *reinterpret_cast<const u32x4 *>(codes + c * PAGE + s0);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) tile[(s0 + i) * LDR + c] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
-    }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int id = j * 256 + (int)threadIdx.x, slot = id / UNITS, u = id % UNITS;
-    if (slot < s.lo || slot >= s.hi) continue;
+  const uint8_t *codes = codes_of(a.c, s.page < 0 ? 0 : s.page, head, task.values);
+  const float scale = s.page < 0 ? 0.0f : *scale_of(a.c, s.page, head, task.values);
+  if (!task.values) {
     int c0, c1;
-    unit_channels<LAYOUT>(u, rot, c0, c1);
-    const int64_t row = row_of(s, slot);
-    float va[8] = {}, vb[8] = {};
-    if (slot < held) {
-      const uint8_t *from = values ? tile + slot * LDR : codes + slot * HD;
-      const u32x2 w0 = *reinterpret_cast<const u32x2 *>(from + c0), w1 = *reinterpret_cast<const u32x2 *>(from + c1);
+    unit_channels<LAYOUT>(task.u, a.rot, c0, c1);
+    u32x2 w[4][2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float t[4];
-        decode4(w0[i], t);
+    for (int j = 0; j < 4; ++j) {
+      const int slot = task.first + 16 * j;
+      w[j][0] = *reinterpret_cast<const u32x2 *>(codes + slot * HD + c0);
+      w[j][1] = *reinterpret_cast<const u32x2 *>(codes + slot * HD + c1);
+    }
 #pragma unroll
-        for (int m = 0; m < 4; ++m) va[4 * i + m] = t[m] * scale;
-        decode4(w1[i], t);
+    for (int j = 0; j < 4; ++j) {
+      const int slot = task.first + 16 * j;
+      if (slot < s.lo || slot >= s.hi) continue;
+      const int64_t row = row_of(s, slot);
+      float v[2][8];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) vb[4 * i + m] = t[m] * scale;
-      }
-      if (16 * u < rot) {
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float t[4];
+          decode4(w[j][e][i], t);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) v[e][4 * i + m] = slot < held ? t[m] * scale : 0.0f;
+        }
+      if (16 * task.u < a.rot) {
         float cs[8], sn[8];
-        load8<float>(a.cos + row * (rot / 2) + 8 * u, cs);
-        load8<float>(a.sin + row * (rot / 2) + 8 * u, sn);
+        load8<float>(a.cos + row * (a.rot / 2) + 8 * task.u, cs);
+        load8<float>(a.sin + row * (a.rot / 2) + 8 * task.u, sn);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sn[i] = -sn[i];
-        rotate_unit<LAYOUT>(va, vb, cs, sn);
+        rotate_unit<LAYOUT>(v[0], v[1], cs, sn);
       }
+      T *p = dst + row * a.ldk;
+      store8<T>(p + c0, v[0]);
+      store8<T>(p + c1, v[1]);
     }
-    T *p = dst + row * ld;
-    store8<T>(p + c0, va);
-    store8<T>(p + c1, vb);
+    return;
+  }
+  if (task.first >= s.hi || task.first + 16 <= s.lo) return;
+  u32x4 w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const u32x4 *>(codes + (task.ch0 + j) * PAGE + task.first);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    // four channels by four tokens, turned
+    const uint32_t lo01 = __builtin_amdgcn_perm(w[1][i], w[0][i], 0x05010400), lo23 = __builtin_amdgcn_perm(w[3][i], w[2][i], 0x05010400);
+    const uint32_t hi01 = __builtin_amdgcn_perm(w[1][i], w[0][i], 0x07030602), hi23 = __builtin_amdgcn_perm(w[3][i], w[2][i], 0x07030602);
+    const uint32_t turned[4] = {__builtin_amdgcn_perm(lo23, lo01, 0x05040100), __builtin_amdgcn_perm(lo23, lo01, 0x07060302),
+                                __builtin_amdgcn_perm(hi23, hi01, 0x05040100), __builtin_amdgcn_perm(hi23, hi01, 0x07060302)};
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const int slot = task.first + 4 * i + m;
+      if (slot < s.lo || slot >= s.hi) continue;
+      float t[4];
+      decode4(turned[m], t);
+      typename Vec4<T>::type v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = (T)(slot < held ? t[j] * scale : 0.0f);
+      *reinterpret_cast<typename Vec4<T>::type *>(dst + row_of(s, slot) * a.ldv + task.ch0) = v;
+    }
   }
 }
 
@@ -235,11 +297,11 @@ int64_t most_pages(int64_t rows, int n_seqs) {
 
 template <bool READ, typename T, int HD> void launch_move(const MoveArgs &a, int layout, dim3 grid, hipStream_t s) {
   if (layout == RVQ_ROPE_HALVES) {
-    if (READ) hipLaunchKernelGGL((cache8_read_kernel<T, HD, RVQ_ROPE_HALVES>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_HALVES>), grid, dim3(256), 0, s, a);
+    if (READ) hipLaunchKernelGGL((cache8_read_kernel<T, HD, RVQ_ROPE_HALVES>), grid, dim3(2 * HD), 0, s, a);
+    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_HALVES>), grid, dim3(2 * HD), 0, s, a);
   } else {
-    if (READ) hipLaunchKernelGGL((cache8_read_kernel<T, HD, RVQ_ROPE_ADJACENT>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_ADJACENT>), grid, dim3(256), 0, s, a);
+    if (READ) hipLaunchKernelGGL((cache8_read_kernel<T, HD, RVQ_ROPE_ADJACENT>), grid, dim3(2 * HD), 0, s, a);
+    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_ADJACENT>), grid, dim3(2 * HD), 0, s, a);
   }
 }
 template <bool READ, typename T> void launch_move_hd(const MoveArgs &a, int layout, dim3 grid, hipStream_t s) {
@@ -248,8 +310,10 @@ template <bool READ, typename T> void launch_move_hd(const MoveArgs &a, int layo
   else launch_move<READ, T, 256>(a, layout, grid, s);
 }
 template <bool READ> int move(const MoveArgs &a, int layout, int32_t dtype, hipStream_t s) {
-  const int64_t blocks = most_pages(a.c.rows, a.c.n_seqs);
-  const dim3 grid((unsigned)blocks, 2 * a.c.heads);
+  // the heads of a page beside each other: their rows are neighbours in memory, and they read the same tables
+  const int64_t blocks = most_pages(a.c.rows, a.c.n_seqs) * a.c.heads;
+  if (blocks > INT32_MAX) return RVQ_EINVAL;
+  const dim3 grid((unsigned)blocks);
   if (dtype == RVQ_F32) launch_move_hd<READ, float>(a, layout, grid, s);
   else if (dtype == RVQ_BF16) launch_move_hd<READ, __bf16>(a, layout, grid, s);
   else launch_move_hd<READ, _Float16>(a, layout, grid, s);

@@ -70,7 +70,7 @@ __device__ __forceinline__ bool find_run(const AttnArgs &a, int64_t w, int64_t &
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d, 64);
   run = run_of(total);
-  return find_piece(a.c.n_seqs, w * run, [&](int i) { return units_of(a, i); }, seq, inside);
+  return find_piece<int64_t>(a.c.n_seqs, w * run, [&](int i) { return units_of(a, i); }, seq, inside);
 }
 
 template <typename T, int HD> struct Columns {

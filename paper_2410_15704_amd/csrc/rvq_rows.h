@@ -18,6 +18,22 @@ template <typename T> struct Vec8;
 template <> struct Vec8<__bf16> { typedef bf16x8 type; };
 template <> struct Vec8<_Float16> { typedef f16x8 type; };
 
+// eight neighbouring elements as they are (16-byte aligned), and as floats
+template <typename T> struct Raw8 { typedef typename Vec8<T>::type type; };
+template <> struct Raw8<float> {
+  struct type { f32x4 a, b; };
+};
+template <typename T> __device__ __forceinline__ typename Raw8<T>::type raw8(const T *p) {
+  return *reinterpret_cast<const typename Raw8<T>::type *>(p);
+}
+template <typename T> __device__ __forceinline__ void widen(const typename Raw8<T>::type &x, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
+}
+template <> __device__ __forceinline__ void widen<float>(const Raw8<float>::type &x, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[i] = x.a[i]; v[4 + i] = x.b[i]; }
+}
 // eight neighbouring elements, 16-byte aligned
 template <typename T> __device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
   const typename Vec8<T>::type x = *reinterpret_cast<const typename Vec8<T>::type *>(p);
