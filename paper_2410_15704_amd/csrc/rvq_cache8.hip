@@ -9,6 +9,8 @@
 // without a transposition).  A thread of the values takes four channels of 16 tokens: its reads and writes of rows are 8 or
 // 16 bytes, neighbours beside each other along the row, and of codes 16 bytes of a channel; what lies between is
 // a transposition of 4 x 4 bytes in registers (reading), or none (the conversion packs neighbouring tokens).
+#include <type_traits>
+
 #include "rvq_cache8.h"
 
 namespace {
@@ -66,113 +68,139 @@ __device__ __forceinline__ uint32_t again4(uint32_t w, float ratio) {
   return encode4_any(v[0] * ratio, v[1] * ratio, v[2] * ratio, v[3] * ratio);
 }
 
-// Keys: 16 channels (unit u) of the four tokens first + 16 j.  Values: channels ch0 .. ch0 + 3 of tokens first .. first + 15.
-template <int HD> struct Task {
+// A thread's part of a page, 4 TOK elements.  Keys: 16 channels (unit u) of the tokens first + j PAGE 4 / TOK, j < TOK / 4.  Values:
+// channels ch0 .. ch0 + 3 of tokens first .. first + TOK - 1.
+template <int HD, int TOK> struct Task {
+  static constexpr int HALF = 16 * HD / TOK;         // threads of the keys, and of the values
+  static constexpr int STEP = HALF / (HD / 16);      // tokens between a thread's keys
   bool values;
   int first, u, ch0;
   __device__ __forceinline__ Task() {
-    const int t = threadIdx.x % HD;
-    values = threadIdx.x >= HD;
+    const int t = threadIdx.x % HALF;
+    values = threadIdx.x >= HALF;
     u = t % (HD / 16);
     ch0 = t % (HD / 4) * 4;
-    first = values ? t / (HD / 4) * 16 : t / (HD / 16);
+    first = values ? t / (HD / 4) * TOK : t / (HD / 16);
   }
 };
 template <typename T> struct Vec4 {
   typedef T type __attribute__((ext_vector_type(4)));
 };
 
-template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) void cache8_append_kernel(const MoveArgs a) {
-  __shared__ float wave_max[2 * HD / 64];
+template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(4 * HD) void cache8_append_kernel(const MoveArgs a) {
+  constexpr int TOK = 8, KEYS = TOK / 4, WAVES_HALF = Task<HD, TOK>::HALF / 64;
+  __shared__ uint32_t wave_max[2 * WAVES_HALF];
   Span s;
   if (!find_span<false>(a, s) || s.page < 0) return;
   const int head = blockIdx.x % a.c.heads;
-  const Task<HD> task;
+  const Task<HD, TOK> task;
   float *scale_at = scale_of(a.c, s.page, head, task.values);
   const float old = s.lo ? *scale_at : 0.0f;
   uint8_t *codes = codes_of(a.c, s.page, head, task.values);
 
-  float x[4][16];  // keys [token][channel], values [channel][token]
-  int c0 = 0, c1 = 0;
-  if (!task.values) {
-    unit_channels<LAYOUT>(task.u, a.rot, c0, c1);
-    const T *src = (const T *)a.k + head * a.hsk;
-    typename Raw8<T>::type va[4], vb[4];
+  float x[4 * TOK];  // keys [token][16 channels], values [4 channels][token]
+  const Unit<LAYOUT> unit(task.u, HD, a.rot);
+  // FULL: the step fills the whole page
+  const auto load = [&](auto full) {
+    constexpr bool FULL = decltype(full)::value;
+    const auto row_at = [&](int slot) { return row_of(s, FULL ? slot : nearest(s, slot)); };
+    if (!task.values) {
+      const T *src = (const T *)a.k + head * a.hsk;
+      typename Raw8<T>::type va[KEYS], vb[KEYS];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const T *p = src + row_of(s, nearest(s, task.first + 16 * j)) * a.ldk;
-      va[j] = raw8<T>(p + c0);
-      vb[j] = raw8<T>(p + c1);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float p[8], q[8];
-      widen<T>(va[j], p);
-      widen<T>(vb[j], q);
-      if (16 * task.u < a.rot) {
-        const int64_t row = row_of(s, nearest(s, task.first + 16 * j));
-        float cs[8], sn[8];
-        load8<float>(a.cos + row * (a.rot / 2) + 8 * task.u, cs);
-        load8<float>(a.sin + row * (a.rot / 2) + 8 * task.u, sn);
-        rotate_unit<LAYOUT>(p, q, cs, sn);
+      for (int j = 0; j < KEYS; ++j) {
+        const T *p = src + row_at(task.first + task.STEP * j) * a.ldk;
+        va[j] = raw8<T>(p + unit.c0);
+        vb[j] = raw8<T>(p + unit.c1);
       }
-      const int slot = task.first + 16 * j;
-      const bool in = slot >= s.lo && slot < s.hi;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[j][i] = in ? p[i] : 0.0f;
-        x[j][8 + i] = in ? q[i] : 0.0f;
+      for (int j = 0; j < KEYS; ++j) {
+        float p[8], q[8];
+        widen<T>(va[j], p);
+        widen<T>(vb[j], q);
+        if (a.rot) {
+          const int64_t row = row_at(task.first + task.STEP * j);
+          float cs[8], sn[8];
+          unit.entries(a.cos + row * (a.rot / 2), cs);
+          unit.entries(a.sin + row * (a.rot / 2), sn);
+          unit.rotate(p, q, cs, sn);
+        }
+        const int slot = task.first + task.STEP * j;
+        const bool in = FULL || (slot >= s.lo && slot < s.hi);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[16 * j + i] = in ? p[i] : 0.0f;
+          x[16 * j + 8 + i] = in ? q[i] : 0.0f;
+        }
       }
+    } else if (FULL || (task.first < s.hi && task.first + TOK > s.lo)) {
+      const T *src = (const T *)a.v + head * a.hsv + task.ch0, *row0 = src + row_at(task.first) * a.ldv;
+      typename Vec4<T>::type v[TOK];
+#pragma unroll
+      for (int i = 0; i < TOK; ++i)
+        v[i] = *reinterpret_cast<const typename Vec4<T>::type *>(FULL ? row0 + i * a.ldv : src + row_at(task.first + i) * a.ldv);
+#pragma unroll
+      for (int i = 0; i < TOK; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[TOK * j + i] = FULL || (task.first + i >= s.lo && task.first + i < s.hi) ? (float)v[i][j] : 0.0f;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4 * TOK; ++i) x[i] = 0.0f;
     }
-  } else if (task.first < s.hi && task.first + 16 > s.lo) {
-    const T *src = (const T *)a.v + head * a.hsv + task.ch0;
-    typename Vec4<T>::type v[16];
+  };
+  if (s.lo == 0 && s.hi == PAGE) load(std::true_type());
+  else load(std::false_type());
+  // Largest magnitude over the workgroup's keys and over its values, as bits (they are ordered like the numbers, infinity and
+  // NaN above all).  Called by all threads.
+  const auto largest = [&](uint32_t mine) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      v[i] = *reinterpret_cast<const typename Vec4<T>::type *>(src + row_of(s, nearest(s, task.first + i)) * a.ldv);
+    for (int d = 32; d; d /= 2) mine = max(mine, (uint32_t)__shfl_xor((int)mine, d, 64));
+    if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = mine;
+    __syncthreads();  // (the first time also: every thread has read the old scale)
+    uint32_t all = 0, own = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int w = 0; w < 2 * WAVES_HALF; ++w) {
+      const uint32_t m = wave_max[w];
+      all = max(all, m);
+      own = (w >= WAVES_HALF) == task.values ? max(own, m) : own;
+    }
+    __syncthreads();
+    return u32x2{all, own};
+  };
+  uint32_t bits = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j][i] = task.first + i >= s.lo && task.first + i < s.hi ? (float)v[i][j] : 0.0f;
-  } else {
+  for (int i = 0; i < 4 * TOK; ++i) bits = max(bits, __float_as_uint(x[i]) & 0x7fffffffu);
+  u32x2 top = largest(bits);
+  const bool finite = __builtin_amdgcn_readfirstlane(top[0]) < 0x7f800000;
+  if (!finite) {  // somewhere: once more without what is not finite
+    bits = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[j][i] = 0.0f;
+    for (int i = 0; i < 4 * TOK; ++i) bits = not_finite(x[i]) ? bits : max(bits, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = largest(bits);
   }
-  float amax = 0.0f;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) amax = not_finite(x[j][i]) ? amax : fmaxf(amax, fabsf(x[j][i]));
-#pragma unroll
-  for (int d = 32; d; d /= 2) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
-  if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = amax;
-  __syncthreads();  // also: every thread has read the old scale
-#pragma unroll
-  for (int w = 0; w < HD / 64; ++w) amax = fmaxf(amax, wave_max[(task.values ? HD / 64 : 0) + w]);
-  float scale = code_scale(amax);
+  float scale = code_scale(__uint_as_float(top[1]));
   scale = s.lo ? fmaxf(scale, old) : scale;
   const bool grown = s.lo && scale > old;
   const float inverse = 1.0f / scale, ratio = grown ? old * inverse : 1.0f;
-  if (threadIdx.x % HD == 0) *scale_at = scale;
+  if (threadIdx.x % task.HALF == 0) *scale_at = scale;
 
-  u32x4 w[4];
+  uint32_t w[TOK];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[j][i] = encode4_any(x[j][4 * i] * inverse, x[j][4 * i + 1] * inverse, x[j][4 * i + 2] * inverse, x[j][4 * i + 3] * inverse);
+  for (int i = 0; i < TOK; ++i) {
+    const float *p = &x[4 * i];
+    if (finite) w[i] = encode4(p[0] * inverse, p[1] * inverse, p[2] * inverse, p[3] * inverse);
+    else w[i] = encode4_any(p[0] * inverse, p[1] * inverse, p[2] * inverse, p[3] * inverse);
+  }
   if (!task.values) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int slot = task.first + 16 * j;
+    for (int j = 0; j < KEYS; ++j) {
+      const int slot = task.first + task.STEP * j;
       if (slot < s.lo || slot >= s.hi) continue;
-      *reinterpret_cast<u32x2 *>(codes + slot * HD + c0) = u32x2{w[j][0], w[j][1]};
-      *reinterpret_cast<u32x2 *>(codes + slot * HD + c1) = u32x2{w[j][2], w[j][3]};
+      *reinterpret_cast<u32x2 *>(codes + slot * HD + unit.c0) = u32x2{w[4 * j], w[4 * j + 1]};
+      *reinterpret_cast<u32x2 *>(codes + slot * HD + unit.c1) = u32x2{w[4 * j + 2], w[4 * j + 3]};
     }
     if (grown)  // the page's earlier tokens
-      for (int at = threadIdx.x * 16; at < s.lo * HD; at += HD * 16) {
+      for (int at = threadIdx.x * 16; at < s.lo * HD; at += task.HALF * 16) {
         u32x4 v = *reinterpret_cast<const u32x4 *>(codes + at);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = again4(v[i], ratio);
@@ -180,24 +208,30 @@ template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) v
       }
     return;
   }
-  // 16 slots of a channel: whole where they are all new; read and written again where old ones change; else the new bytes alone
+  // TOK slots of a channel: whole where they are all new; read and written again where old ones change; else the new bytes alone
   const int from = s.lo - task.first, to = s.hi - task.first;
-  if (from <= 0 && to >= 16) {
+  typedef uint32_t Words __attribute__((ext_vector_type(TOK / 4)));
+  if (from <= 0 && to >= TOK) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4 *>(codes + (task.ch0 + j) * PAGE + task.first) = w[j];
+    for (int j = 0; j < 4; ++j) {
+      Words v;
+#pragma unroll
+      for (int i = 0; i < TOK / 4; ++i) v[i] = w[j * TOK / 4 + i];
+      *reinterpret_cast<Words *>(codes + (task.ch0 + j) * PAGE + task.first) = v;
+    }
   } else if (grown && from > 0) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      u32x4 *at = reinterpret_cast<u32x4 *>(codes + (task.ch0 + j) * PAGE + task.first);
-      u32x4 v = *at;
+      Words *at = reinterpret_cast<Words *>(codes + (task.ch0 + j) * PAGE + task.first);
+      Words v = *at;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < TOK / 4; ++i) {
         const uint32_t more = again4(v[i], ratio);
         uint32_t put = 0;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           const int slot = 4 * i + b;
-          put |= (slot < from ? more : slot < to ? w[j][i] : v[i]) & (0xffu << (8 * b));
+          put |= (slot < from ? more : slot < to ? w[j * TOK / 4 + i] : v[i]) & (0xffu << (8 * b));
         }
         v[i] = put;
       }
@@ -205,10 +239,10 @@ template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) v
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int i = 0; i < TOK; ++i)
       if (i >= from && i < to)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) codes[(task.ch0 + j) * PAGE + task.first + i] = (uint8_t)(w[j][i >> 2] >> (8 * (i & 3)));
+        for (int j = 0; j < 4; ++j) codes[(task.ch0 + j) * PAGE + task.first + i] = (uint8_t)(w[j * TOK / 4 + (i >> 2)] >> (8 * (i & 3)));
   }
 }
 
@@ -216,7 +250,7 @@ template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) v
   Span s;
   if (!find_span<true>(a, s)) return;
   const int head = blockIdx.x % a.c.heads;
-  const Task<HD> task;
+  const Task<HD, 16> task;
   T *dst = (T *)(task.values ? a.v : a.k);
   if (!dst) return;
   dst += head * (task.values ? a.hsv : a.hsk);
@@ -225,68 +259,76 @@ template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) v
   const int held = s.page < 0 ? 0 : (int)(end < 0 ? 0 : end > PAGE ? PAGE : end);
   const uint8_t *codes = codes_of(a.c, s.page < 0 ? 0 : s.page, head, task.values);
   const float scale = s.page < 0 ? 0.0f : *scale_of(a.c, s.page, head, task.values);
-  if (!task.values) {
-    int c0, c1;
-    unit_channels<LAYOUT>(task.u, a.rot, c0, c1);
-    u32x2 w[4][2];
+  // FULL: the step takes the whole page, and all of it is there
+  const auto move_page = [&](auto full) {
+    constexpr bool FULL = decltype(full)::value;
+    const auto wanted = [&](int slot) { return FULL || (slot >= s.lo && slot < s.hi); };
+    const auto there = [&](int slot) { return FULL || slot < held; };
+    if (!task.values) {
+      const Unit<LAYOUT> unit(task.u, HD, a.rot);
+      u32x2 w[4][2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int slot = task.first + 16 * j;
-      w[j][0] = *reinterpret_cast<const u32x2 *>(codes + slot * HD + c0);
-      w[j][1] = *reinterpret_cast<const u32x2 *>(codes + slot * HD + c1);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int slot = task.first + 16 * j;
-      if (slot < s.lo || slot >= s.hi) continue;
-      const int64_t row = row_of(s, slot);
-      float v[2][8];
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float t[4];
-          decode4(w[j][e][i], t);
-#pragma unroll
-          for (int m = 0; m < 4; ++m) v[e][4 * i + m] = slot < held ? t[m] * scale : 0.0f;
-        }
-      if (16 * task.u < a.rot) {
-        float cs[8], sn[8];
-        load8<float>(a.cos + row * (a.rot / 2) + 8 * task.u, cs);
-        load8<float>(a.sin + row * (a.rot / 2) + 8 * task.u, sn);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sn[i] = -sn[i];
-        rotate_unit<LAYOUT>(v[0], v[1], cs, sn);
+      for (int j = 0; j < 4; ++j) {
+        const uint8_t *at = codes + (task.first + 16 * j) * HD;
+        w[j][0] = *reinterpret_cast<const u32x2 *>(at + unit.c0);
+        w[j][1] = *reinterpret_cast<const u32x2 *>(at + unit.c1);
       }
-      T *p = dst + row * a.ldk;
-      store8<T>(p + c0, v[0]);
-      store8<T>(p + c1, v[1]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int slot = task.first + 16 * j;
+        if (!wanted(slot)) continue;
+        const int64_t row = row_of(s, slot);
+        float v[2][8];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float t[4];
+            decode4(w[j][e][i], t);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) v[e][4 * i + m] = there(slot) ? t[m] * scale : 0.0f;
+          }
+        if (a.rot) {
+          float cs[8], sn[8];
+          unit.entries(a.cos + row * (a.rot / 2), cs);
+          unit.entries(a.sin + row * (a.rot / 2), sn);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sn[i] = -sn[i];
+          unit.rotate(v[0], v[1], cs, sn);
+        }
+        T *p = dst + row * a.ldk;
+        store8<T>(p + unit.c0, v[0]);
+        store8<T>(p + unit.c1, v[1]);
+      }
+      return;
     }
-    return;
-  }
-  if (task.first >= s.hi || task.first + 16 <= s.lo) return;
-  u32x4 w[4];
+    if (!FULL && (task.first >= s.hi || task.first + 16 <= s.lo)) return;
+    u32x4 w[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const u32x4 *>(codes + (task.ch0 + j) * PAGE + task.first);
+    for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const u32x4 *>(codes + (task.ch0 + j) * PAGE + task.first);
+    T *row0 = dst + row_of(s, task.first) * a.ldv + task.ch0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    // four channels by four tokens, turned
-    const uint32_t lo01 = __builtin_amdgcn_perm(w[1][i], w[0][i], 0x05010400), lo23 = __builtin_amdgcn_perm(w[3][i], w[2][i], 0x05010400);
-    const uint32_t hi01 = __builtin_amdgcn_perm(w[1][i], w[0][i], 0x07030602), hi23 = __builtin_amdgcn_perm(w[3][i], w[2][i], 0x07030602);
-    const uint32_t turned[4] = {__builtin_amdgcn_perm(lo23, lo01, 0x05040100), __builtin_amdgcn_perm(lo23, lo01, 0x07060302),
-                                __builtin_amdgcn_perm(hi23, hi01, 0x05040100), __builtin_amdgcn_perm(hi23, hi01, 0x07060302)};
+    for (int i = 0; i < 4; ++i) {
+      // four channels by four tokens, turned
+      const uint32_t lo01 = __builtin_amdgcn_perm(w[1][i], w[0][i], 0x05010400), lo23 = __builtin_amdgcn_perm(w[3][i], w[2][i], 0x05010400);
+      const uint32_t hi01 = __builtin_amdgcn_perm(w[1][i], w[0][i], 0x07030602), hi23 = __builtin_amdgcn_perm(w[3][i], w[2][i], 0x07030602);
+      const uint32_t turned[4] = {__builtin_amdgcn_perm(lo23, lo01, 0x05040100), __builtin_amdgcn_perm(lo23, lo01, 0x07060302),
+                                  __builtin_amdgcn_perm(hi23, hi01, 0x05040100), __builtin_amdgcn_perm(hi23, hi01, 0x07060302)};
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const int slot = task.first + 4 * i + m;
-      if (slot < s.lo || slot >= s.hi) continue;
-      float t[4];
-      decode4(turned[m], t);
-      typename Vec4<T>::type v;
+      for (int m = 0; m < 4; ++m) {
+        const int slot = task.first + 4 * i + m;
+        if (!wanted(slot)) continue;
+        float t[4];
+        decode4(turned[m], t);
+        typename Vec4<T>::type v;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = (T)(slot < held ? t[j] * scale : 0.0f);
-      *reinterpret_cast<typename Vec4<T>::type *>(dst + row_of(s, slot) * a.ldv + task.ch0) = v;
+        for (int j = 0; j < 4; ++j) v[j] = (T)(there(slot) ? t[j] * scale : 0.0f);
+        *reinterpret_cast<typename Vec4<T>::type *>(row0 + (4 * i + m) * a.ldv) = v;
+      }
     }
-  }
+  };
+  if (s.lo == 0 && s.hi == PAGE && held == PAGE) move_page(std::true_type());
+  else move_page(std::false_type());
 }
 
 // pages that `rows` rows of n_seqs sequences can span: floor((n + 62) / 64) + 1 for each of n >= 1 rows
@@ -298,10 +340,10 @@ int64_t most_pages(int64_t rows, int n_seqs) {
 template <bool READ, typename T, int HD> void launch_move(const MoveArgs &a, int layout, dim3 grid, hipStream_t s) {
   if (layout == RVQ_ROPE_HALVES) {
     if (READ) hipLaunchKernelGGL((cache8_read_kernel<T, HD, RVQ_ROPE_HALVES>), grid, dim3(2 * HD), 0, s, a);
-    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_HALVES>), grid, dim3(2 * HD), 0, s, a);
+    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_HALVES>), grid, dim3(4 * HD), 0, s, a);
   } else {
     if (READ) hipLaunchKernelGGL((cache8_read_kernel<T, HD, RVQ_ROPE_ADJACENT>), grid, dim3(2 * HD), 0, s, a);
-    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_ADJACENT>), grid, dim3(2 * HD), 0, s, a);
+    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_ADJACENT>), grid, dim3(4 * HD), 0, s, a);
   }
 }
 template <bool READ, typename T> void launch_move_hd(const MoveArgs &a, int layout, dim3 grid, hipStream_t s) {

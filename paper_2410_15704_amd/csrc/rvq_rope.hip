@@ -66,24 +66,20 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a, int hgroups
   const int r = threadIdx.x / tpr, t = threadIdx.x - r * tpr;
   if (r >= rows_per_block) return;
   const int h0 = t / units, u = t - h0 * units;
-  int c0, c1;
-  unit_channels<LAYOUT>(u, a.rot, c0, c1);
-  const bool turns = 16 * u < a.rot;
+  const Unit<LAYOUT> unit(u, a.hd, a.rot);
   for (int64_t n = (int64_t)blockIdx.x * rows_per_block + r; n < a.N; n += (int64_t)gridDim.x * rows_per_block) {
     float cs[8], sn[8];
-    if (turns) {
-      load8<float>(a.cos + n * (a.rot / 2) + 8 * u, cs);
-      load8<float>(a.sin + n * (a.rot / 2) + 8 * u, sn);
-    }
+    unit.entries(a.cos + n * (a.rot / 2), cs);
+    unit.entries(a.sin + n * (a.rot / 2), sn);
     for (int h = h0; h < a.heads; h += hgroups) {
       const T *x = (const T *)a.x + n * a.ldx + h * a.hsx;
       T *o = (T *)a.out + n * a.ldo + h * a.hso;
       float p[8], q[8];
-      load8<T>(x + c0, p);
-      load8<T>(x + c1, q);
-      if (turns) rotate_unit<LAYOUT>(p, q, cs, sn);
-      store8<T>(o + c0, p);
-      store8<T>(o + c1, q);
+      load8<T>(x + unit.c0, p);
+      load8<T>(x + unit.c1, q);
+      unit.rotate(p, q, cs, sn);
+      store8<T>(o + unit.c0, p);
+      store8<T>(o + unit.c1, q);
     }
   }
 }

@@ -60,18 +60,6 @@ template <> __device__ __forceinline__ void store8<float>(float *p, const float 
   reinterpret_cast<f32x4 *>(p)[1] = b;
 }
 
-// A unit of a head is 16 channels whose rotation needs nothing else: two groups of eight that begin at c0
-// and c1.  Units below rot / 16 hold the pairs 8 u .. 8 u + 7, the others are channels that do not rotate.
-template <int LAYOUT> __device__ __forceinline__ void unit_channels(int u, int rot, int &c0, int &c1) {
-  if (LAYOUT == RVQ_ROPE_HALVES && 16 * u < rot) {
-    c0 = 8 * u;
-    c1 = rot / 2 + 8 * u;
-  } else {
-    c0 = 16 * u;
-    c1 = c0 + 8;
-  }
-}
-
 // One pair in fp32: a product, then a multiply-add, written out so that every kernel rounds alike; the empty statements
 // keep the compiler from taking the conversion to a 16-bit type into the multiply-add (fp16 would then skip the fp32 rounding).
 __device__ __forceinline__ void rotate_pair(float &a, float &b, float c, float s) {
@@ -82,19 +70,49 @@ __device__ __forceinline__ void rotate_pair(float &a, float &b, float c, float s
   asm("" : "+v"(b));
 }
 
-// the rotation of a unit
-template <int LAYOUT>
-__device__ __forceinline__ void rotate_unit(float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8]) {
-  if constexpr (LAYOUT == RVQ_ROPE_HALVES) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) rotate_pair(a[i], b[i], cs[i], sn[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      rotate_pair(a[2 * i], a[2 * i + 1], cs[i], sn[i]);
-      rotate_pair(b[2 * i], b[2 * i + 1], cs[4 + i], sn[4 + i]);
+// A unit of a head is 16 channels whose rotation needs nothing else: two groups of eight that begin at c0 and c1.
+//   adjacent pairs  the u-th group of each half of the head, four pairs in each: the groups of neighbouring units lie beside
+//                   each other in memory
+//   halves          the u-th groups of the two halves of what rotates, eight pairs; then 16 neighbouring channels of the rest
+// Both need rot and the head's channels in multiples of 16.
+template <int LAYOUT> struct Unit {
+  int c0, c1, u;
+  bool turn0, turn1;
+  __device__ __forceinline__ Unit(int unit, int hd, int rot) : u(unit) {
+    if (LAYOUT == RVQ_ROPE_HALVES) {
+      const bool turns = 16 * u < rot;
+      c0 = turns ? 8 * u : 16 * u;
+      c1 = c0 + (turns ? rot / 2 : 8);
+      turn0 = turn1 = turns;
+    } else {
+      c0 = 8 * u;
+      c1 = hd / 2 + 8 * u;
+      turn0 = c0 < rot;
+      turn1 = c1 < rot;
     }
   }
-}
+  // the entries of a row of tables [.][rot / 2]
+  __device__ __forceinline__ void entries(const float *row, float (&e)[8]) const {
+    const int p0 = LAYOUT == RVQ_ROPE_HALVES ? 8 * u : c0 / 2, p1 = LAYOUT == RVQ_ROPE_HALVES ? 8 * u + 4 : c1 / 2;
+    // (of a unit that does not turn: the first entries, not used; a load under a condition costs more)
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(row + (turn0 ? p0 : 0)), b = *reinterpret_cast<const f32x4 *>(row + (turn1 ? p1 : 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { e[i] = a[i]; e[4 + i] = b[i]; }
+  }
+  __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8]) const {
+    if constexpr (LAYOUT == RVQ_ROPE_HALVES) {
+      if (!turn0) return;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rotate_pair(a[i], b[i], cs[i], sn[i]);
+    } else {
+      if (turn0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rotate_pair(a[2 * i], a[2 * i + 1], cs[i], sn[i]);
+      if (turn1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rotate_pair(b[2 * i], b[2 * i + 1], cs[4 + i], sn[4 + i]);
+    }
+  }
+};
 
 }  // namespace
