@@ -388,9 +388,11 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_ker
   }
 }
 
-// Joins the parts of the item that begins in run blockIdx.x and goes on, column by column: the first part lies at H_FIRST, the
-// others at the beginnings of the following runs.  Maxima and sums of all parts are fetched together, then each wavefront adds up
-// a quarter of the parts, the first few of them requested along with the maxima.
+// Joins the parts of the item that begins in run blockIdx.x and goes on: the first part lies at H_FIRST, the others at the
+// beginnings of the following runs.  Up to eight parts (a batch of sequences: an item meets few runs) take a wavefront per column, which
+// asks for all of them at once; more (one long cache) a workgroup per column: maxima and sums are fetched together, then each
+// wavefront adds up a quarter of the parts, the first few requested along with the maxima.  (64 parts of 32 columns 7.0 us, of
+// which 3.9 are what the launch takes with nothing to join; by one wavefront 9.)
 constexpr int MOST_GROUPS = 1024;
 template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void cache8_join_kernel(const AttnArgs a) {
   __shared__ float sh_w[MOST_GROUPS + 1], sh_red[8];
@@ -400,22 +402,58 @@ template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void 
   const int parts = (int)hd[H_PARTS], cols = (int)hd[H_COLS], slot0 = (int)hd[H_FIRST];
   if (!parts) return;
   typedef float Out __attribute__((ext_vector_type(HD / 64)));  // a lane's channels
-  for (int c = blockIdx.y; c < cols; c += gridDim.y) {
-    const auto part = [&](int i) { return a.part + ((int64_t)(i ? 2 * (w + i) : slot0) * WIDTH + c) * (HD + 2); };
-    const auto values = [&](int i) {
-      const float *p = part(i) + lane * (HD / 64);
-      Out o;
+  const auto part = [&](int i, int c) { return a.part + ((int64_t)(i ? 2 * (w + i) : slot0) * WIDTH + c) * (HD + 2); };
+  const auto values = [&](int i, int c) {
+    const float *p = part(i, c) + lane * (HD / 64);
+    Out o;
 #pragma unroll
-      for (int j = 0; j < HD / 64; ++j) o[j] = p[j];
-      return o;
-    };
-    constexpr int EARLY = 4;
+    for (int j = 0; j < HD / 64; ++j) o[j] = p[j];
+    return o;
+  };
+  const auto out_at = [&](int c) {
+    const uint32_t col = (uint32_t)hd[H_COL0] + c, token = col / (uint32_t)a.rep;
+    const int64_t h = hd[H_HEAD] * a.rep + (col - token * a.rep);
+    return (T *)a.out + (hd[H_ROW] + token) * a.ldo + h * a.hso;
+  };
+  constexpr int FEW = 8;
+  if (parts <= FEW) {
+    for (int c = blockIdx.y * 4 + wave; c < cols; c += gridDim.y * 4) {
+      Out v[FEW];
+      float m[FEW], l[FEW], top = NEG, sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < FEW; ++i) {
+        const int at = min(i, parts - 1);
+        m[i] = part(at, c)[HD];
+        l[i] = part(at, c)[HD + 1];
+        v[i] = values(at, c);
+      }
+#pragma unroll
+      for (int i = 0; i < FEW; ++i) top = fmaxf(top, m[i]);
+      Out o = {};
+#pragma unroll
+      for (int i = 0; i < FEW; ++i)
+        if (i < parts) {
+          const float x = __builtin_amdgcn_exp2f(m[i] - top);
+          sum += x * l[i];
+          o += x * v[i];
+        }
+      T *out = out_at(c) + lane * (HD / 64);
+      const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+      for (int j = 0; j < HD / 64; ++j) out[j] = (T)(sum != 0.0f ? o[j] * over : 0.0f);
+    }
+    return;
+  }
+  for (int c = blockIdx.y; c < cols; c += gridDim.y) {
+    constexpr int EARLY = 8;
     Out early[EARLY];
 #pragma unroll
-    for (int e = 0; e < EARLY; ++e) early[e] = wave + 4 * e < parts ? values(wave + 4 * e) : Out{};
-    float top = NEG;
+    for (int e = 0; e < EARLY; ++e) early[e] = values(min(wave + 4 * e, parts - 1), c);
+    float top = NEG, l0 = 0.0f;
     for (int i = t; i < parts; i += 256) {
-      const float m = part(i)[HD];
+      const float *p = part(i, c) + HD;
+      const float m = p[0];
+      if (i == t) l0 = p[1];
       sh_w[i] = m;
       top = fmaxf(top, m);
     }
@@ -428,7 +466,7 @@ template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void 
     for (int i = t; i < parts; i += 256) {
       const float x = __builtin_amdgcn_exp2f(sh_w[i] - top);
       sh_w[i] = x;
-      sum += x * part(i)[HD + 1];
+      sum += x * (i == t ? l0 : part(i, c)[HD + 1]);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
@@ -438,18 +476,15 @@ template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void 
 #pragma unroll
     for (int e = 0; e < EARLY; ++e)
       if (wave + 4 * e < parts) o += sh_w[wave + 4 * e] * early[e];
-#pragma unroll 8
-    for (int i = wave + 4 * EARLY; i < parts; i += 4) o += sh_w[i] * values(i);
+#pragma unroll 4
+    for (int i = wave + 4 * EARLY; i < parts; i += 4) o += sh_w[i] * values(i, c);
 #pragma unroll
     for (int j = 0; j < HD / 64; ++j) sh_o[wave][lane * (HD / 64) + j] = o[j];
     __syncthreads();
     if (t < HD) {
       sum = (sh_red[4] + sh_red[5]) + (sh_red[6] + sh_red[7]);
       const float x = (sh_o[0][t] + sh_o[1][t]) + (sh_o[2][t] + sh_o[3][t]);
-      const uint32_t col = (uint32_t)hd[H_COL0] + c, token = col / (uint32_t)a.rep;
-      const int64_t h = hd[H_HEAD] * a.rep + (col - token * a.rep);
-      T *out = (T *)a.out + (hd[H_ROW] + token) * a.ldo + h * a.hso;
-      out[t] = (T)(sum != 0.0f ? x * (1.0f / sum) : 0.0f);
+      out_at(c)[t] = (T)(sum != 0.0f ? x * (1.0f / sum) : 0.0f);
     }
     __syncthreads();
   }
