@@ -12,7 +12,6 @@ struct AttnArgs {
   float scale;      // log2(e) times the softmax scale
   float *part;      // [2 * workgroups][COLS or MANY][HD + 2]
   int64_t *header;  // [workgroups][8]
-  int64_t least;    // fewest units of a workgroup
 };
 
 // the kernel for many columns; half: fp16 queries, else bf16; whole: a workgroup takes one item

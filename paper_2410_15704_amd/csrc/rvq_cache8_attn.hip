@@ -44,7 +44,7 @@ __device__ __forceinline__ bool find_run(const AttnArgs &a, int64_t w, int64_t &
   const int lane = threadIdx.x & 63;
   const auto run_of = [&](int64_t total) {
     const int64_t even = (total + gridDim.x - 1) / gridDim.x;
-    return even > a.least ? even : a.least;
+    return even > WAVES ? even : WAVES;  // a page for every wavefront
   };
   if (a.c.n_seqs <= 64) {
     const int64_t units = lane < a.c.n_seqs ? units_of(a, lane) : 0;
@@ -309,22 +309,15 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_ker
         if (t && (t & 63) == 0) ids = read_ids(t);
         return __builtin_amdgcn_readlane(ids, t & 63);
       };
-      // While a page is worked on the next one's codes are on their way, where registers hold two.
-      constexpr bool TWO = HD == 64;
-      PageCodes<HD> even, odd;
+      PageCodes<HD> codes;
       int page = id_at(0);
-      if (page >= 0) even.load(a, page, head);
+      if (page >= 0) codes.load(a, page, head);  // on their way while the columns are made
       make_columns<T, HD>(a, s, k, raw, c);
-      const auto step = [&](int t, PageCodes<HD> &here, PageCodes<HD> &ahead) {
-        const int t0 = first_token(t), now = page;
+      for (int t = 0; t < count; ++t) {
+        const int t0 = first_token(t);
+        if (page >= 0) take_page<T, HD>(a, c, st, codes, t0, all_see(a, s, k, t0));
         page = id_at(t + 1);
-        if (TWO && page >= 0) ahead.load(a, page, head);
-        if (now >= 0) take_page<T, HD>(a, c, st, here, t0, all_see(a, s, k, t0));
-        if (!TWO && page >= 0) here.load(a, page, head);
-      };
-      for (int t = 0; t < count; t += TWO ? 2 : 1) {
-        step(t, even, odd);
-        if (TWO && t + 1 < count) step(t + 1, odd, even);
+        if (page >= 0) codes.load(a, page, head);
       }
       // the wavefronts' results together
       st.l += __shfl_xor(st.l, 16, 64);
@@ -437,6 +430,38 @@ template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void 
           sum += x * l[i];
           o += x * v[i];
         }
+      T *out = out_at(c) + lane * (HD / 64);
+      const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+      for (int j = 0; j < HD / 64; ++j) out[j] = (T)(sum != 0.0f ? o[j] * over : 0.0f);
+    }
+    return;
+  }
+  if (WIDTH == MANY) {
+    for (int c = blockIdx.y * 4 + wave; c < cols; c += gridDim.y * 4) {
+      float top = NEG, sum = 0.0f;
+      for (int i = lane; i < parts; i += 64) top = fmaxf(top, part(i, c)[HD]);
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+      Out o = {};
+      for (int i0 = 0; i0 < parts; i0 += 64) {
+        float x = 0.0f;  // the weight of a lane's part
+        if (i0 + lane < parts) {
+          x = __builtin_amdgcn_exp2f(part(i0 + lane, c)[HD] - top);
+          sum += x * part(i0 + lane, c)[HD + 1];
+        }
+        const int some = min(64, parts - i0);
+        for (int i = 0; i < some; i += FEW) {
+          Out v[FEW];
+#pragma unroll
+          for (int e = 0; e < FEW; ++e) v[e] = values(i0 + min(i + e, some - 1), c);
+#pragma unroll
+          for (int e = 0; e < FEW; ++e)
+            if (i + e < some) o += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), (i + e) & 63)) * v[e];
+        }
+      }
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
       T *out = out_at(c) + lane * (HD / 64);
       const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
@@ -580,7 +605,6 @@ int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int6
   a.header = (int64_t *)dWorkspace;
   const Plan p = plan_of(cus, dtype, rows, cache->n_seqs, cache->n_kv_heads, a.rep, hd);
   a.part = (float *)((char *)dWorkspace + p.groups * 64);
-  a.least = p.many ? 1 : WAVES;
   if (dtype == RVQ_F32) launch_attn_hd<float>(a, p, (hipStream_t)stream);
   else if (dtype == RVQ_BF16) launch_attn_hd<__bf16>(a, p, (hipStream_t)stream);
   else launch_attn_hd<_Float16>(a, p, (hipStream_t)stream);

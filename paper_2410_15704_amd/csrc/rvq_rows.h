@@ -60,12 +60,16 @@ template <> __device__ __forceinline__ void store8<float>(float *p, const float 
   reinterpret_cast<f32x4 *>(p)[1] = b;
 }
 
-// One pair in fp32: a product, then a multiply-add, written out so that every kernel rounds alike; the empty statements
-// keep the compiler from taking the conversion to a 16-bit type into the multiply-add (fp16 would then skip the fp32 rounding).
+// One pair in fp32, right to about a unit of the result's last place: what the first product's rounding lost is added again
+// (a difference of products would otherwise lose as many places as it cancels, and a code of three bits behind the leading one,
+// whatever its size, sees that).  Written out so that every kernel rounds alike; the empty statements keep the compiler from
+// taking a conversion to a 16-bit type into the last addition (fp16 would then skip the fp32 rounding).
 __device__ __forceinline__ void rotate_pair(float &a, float &b, float c, float s) {
   const float x = a, y = b;
-  a = fmaf(x, c, -(y * s));
-  b = fmaf(x, s, y * c);
+  const float ys = y * s, yc = y * c;
+  const float lost_s = fmaf(-y, s, ys), lost_c = fmaf(y, c, -yc);
+  a = fmaf(x, c, -ys) + lost_s;
+  b = fmaf(x, s, yc) + lost_c;
   asm("" : "+v"(a));
   asm("" : "+v"(b));
 }
