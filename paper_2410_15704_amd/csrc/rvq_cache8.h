@@ -112,7 +112,8 @@ inline bool rvq_cache8_pointers_ok(const rvq_cache8 *c) {
 // rows of [rows][heads][hd] that are moved 16 bytes at a time
 inline bool rvq_rows16_ok(const void *p, int32_t dtype, int64_t rows, int64_t heads, int64_t hd, int64_t ld, int64_t hs) {
   const int64_t e = dtype == RVQ_F32 ? 4 : 2;
-  return rvq_aligned(p, 16) && rvq_rows_fit(rows, heads, hd, ld, hs) && ((ld | hs) * e) % 16 == 0;
+  if (!rvq_aligned(p, 16) || !rvq_rows_fit(rows, heads, hd, ld, hs)) return false;
+  return ((rows > 1 ? ld : 0) * e) % 16 == 0 && ((heads > 1 ? hs : 0) * e) % 16 == 0;  // one row, one head: no stride
 }
 namespace {
 inline CacheView view_of(const rvq_cache8 *c, const int32_t *cu, int64_t rows) {

@@ -10,12 +10,14 @@ struct AttnArgs {
   int64_t ldq, hsq, ldo, hso;
   int rep, window, sinks;
   float scale;      // log2(e) times the softmax scale
-  float *part;      // [2 * workgroups][COLS or MANY][HD + 2]
-  int64_t *header;  // [workgroups][8]
+  float *part;      // [2 * groups][COLS or MANY][HD + 2]
+  int64_t *header;  // [groups][8]
+  int groups;       // workgroups that share the pages in equal runs
 };
 
-// the kernel for many columns; half: fp16 queries, else bf16; whole: a workgroup takes one item
-void rvq_launch_cache8_chunk(const AttnArgs &a, bool half, int64_t groups, bool whole, hipStream_t s);
+// the kernel for many columns; half: fp16 queries, else bf16
+enum ItemPlan { ITEMS_RUNS, ITEMS_WHOLE, ITEMS_EITHER };
+void rvq_launch_cache8_chunk(const AttnArgs &a, bool half, int64_t grid, ItemPlan items, hipStream_t s);
 
 namespace {
 

@@ -244,7 +244,7 @@ __device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD
       d = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(mark[2], mark[3]), __builtin_bit_cast(f16x8, ones[1]), d, 0, 0, 0);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (d[r] > 0.0f) st.acc[t][r] = __uint_as_float(0x7fc00000u);
+        st.acc[t][r] = __uint_as_float(d[r] > 0.0f ? 0x7fc00000u : __float_as_uint(st.acc[t][r]));
     }
   }
 #pragma unroll
@@ -525,10 +525,16 @@ int attn_cus() {
 }
 
 // How a call is run, from what the host knows: rows, sequences and heads, not the lengths.
+//   Up to 32 columns a sequence (on the average): the kernel for few columns, which reads a page for every 16; 16 sequences of 4000
+//   tokens, us few : many, 16 columns 35 : 52, 32 columns 53 : 57, 36 columns (three readings) 68 : 58.  fp32 queries always.
+//   Many columns: whole items where there is one for every workgroup that fits the chip, which shares nothing (2048 tokens behind
+//   4000, us in runs : whole items 213 : 178, 16384 behind nothing 2221 : 1993); the search for an item's block goes through all
+//   blocks for each item, so not beyond 4096 of them or 1024 sequences.  Fewer items: the lengths decide, on the device.
 struct Plan {
-  bool many;       // the kernel for many columns
-  bool whole;      // its form in which a workgroup takes one item
-  int64_t groups;  // workgroups
+  bool many;
+  ItemPlan items;
+  int groups;    // workgroups of equal runs
+  int64_t grid;  // and all workgroups
 };
 Plan plan_of(int cus, int32_t dtype, int64_t rows, int n_seqs, int heads, int rep, int hd) {
   Plan p;
@@ -536,18 +542,27 @@ Plan plan_of(int cus, int32_t dtype, int64_t rows, int n_seqs, int heads, int re
   p.many = dtype != RVQ_F32 && cols > 2 * COLS * seqs;
   const int per_cu = p.many && hd == 256 ? 1 : 2;
   p.groups = per_cu * cus < MOST_GROUPS ? per_cu * cus : MOST_GROUPS;
-  const int64_t items = cols / MANY * heads;  // at least
-  p.whole = p.many && items >= 2 * p.groups && (cols / MANY + seqs) * heads <= INT32_MAX;
-  if (p.whole) p.groups = (cols / MANY + seqs) * heads;
+  p.grid = p.groups;
+  p.items = ITEMS_RUNS;
+  const int64_t least = cols / MANY * heads, most = (cols / MANY + seqs) * heads;  // items
+  constexpr int MOST_SEQS = 1024, MOST_BLOCKS = 4096;
+  if (!p.many || n_seqs > MOST_SEQS || cols / MANY + seqs > MOST_BLOCKS) return p;
+  if (least >= p.groups) {
+    p.items = ITEMS_WHOLE;
+    p.grid = most;
+  } else if (most <= 2 * p.groups) {
+    p.items = ITEMS_EITHER;
+    if (most > p.grid) p.grid = most;
+  }
   return p;
 }
 
 template <typename T, int HD> void launch_attn(const AttnArgs &a, const Plan &p, hipStream_t s) {
-  const dim3 grid((unsigned)p.groups);
+  const dim3 grid((unsigned)p.groups);  // of the joining kernel, and of equal runs
   if constexpr (!std::is_same<T, float>::value) {
     if (p.many) {
-      rvq_launch_cache8_chunk(a, std::is_same<T, _Float16>::value, p.groups, p.whole, s);
-      if (!p.whole) hipLaunchKernelGGL((cache8_join_kernel<T, HD, MANY>), dim3(grid.x, 16), dim3(256), 0, s, a);
+      rvq_launch_cache8_chunk(a, std::is_same<T, _Float16>::value, p.grid, p.items, s);
+      if (p.items != ITEMS_WHOLE) hipLaunchKernelGGL((cache8_join_kernel<T, HD, MANY>), dim3(grid.x, 16), dim3(256), 0, s, a);
       return;
     }
   }
@@ -576,8 +591,8 @@ int64_t rvq_cache8_attn_workspace_bytes(const rvq_cache8 *cache, int32_t dtype, 
   if (!attn_ok(cache, dtype, rows, n_q_heads)) return 0;
   const int cus = attn_cus();
   const Plan p = plan_of(cus, dtype, rows, cache->n_seqs, cache->n_kv_heads, n_q_heads / cache->n_kv_heads, cache->head_dim);
-  if (p.whole || rows == 0) return 16;
-  return p.groups * 64 + 2 * p.groups * (p.many ? MANY : COLS) * (cache->head_dim + 2) * (int64_t)sizeof(float);
+  if (p.items == ITEMS_WHOLE || rows == 0) return 16;
+  return p.groups * (int64_t)64 + 2 * (int64_t)p.groups * (p.many ? MANY : COLS) * (cache->head_dim + 2) * (int64_t)sizeof(float);
 }
 
 int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int64_t rows, int32_t n_q_heads,
@@ -604,7 +619,8 @@ int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int6
   a.scale = scale * 1.44269504088896340736f;
   a.header = (int64_t *)dWorkspace;
   const Plan p = plan_of(cus, dtype, rows, cache->n_seqs, cache->n_kv_heads, a.rep, hd);
-  a.part = (float *)((char *)dWorkspace + p.groups * 64);
+  a.groups = p.groups;
+  a.part = (float *)((char *)dWorkspace + (int64_t)p.groups * 64);
   if (dtype == RVQ_F32) launch_attn_hd<float>(a, p, (hipStream_t)stream);
   else if (dtype == RVQ_BF16) launch_attn_hd<__bf16>(a, p, (hipStream_t)stream);
   else launch_attn_hd<_Float16>(a, p, (hipStream_t)stream);

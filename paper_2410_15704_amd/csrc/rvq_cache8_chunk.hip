@@ -91,33 +91,59 @@ template <typename Visit> __device__ __forceinline__ void walk(const AttnArgs &a
   }
 }
 
+// What a call's blocks amount to, for one kv head: pages, blocks, pages of the longest one.
+struct Sums {
+  int64_t pages;
+  int blocks, longest;
+};
+__device__ __forceinline__ Sums sum_blocks(const AttnArgs &a, Shared &sh) {
+  Sums s = {0, 0, 0};
+  int64_t pages = 0;
+  int blocks = 0, longest = 0;
+  walk(a, sh, [&](const Place &p) {
+    pages += p.pages;
+    blocks += p.pages != 0;
+    longest = max(longest, p.pages);
+    return false;
+  });
+  (void)scan256(pages, sh.wave64, s.pages);
+  (void)scan256(blocks, sh.wave, s.blocks);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d, 64));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh.wave[threadIdx.x >> 6] = longest;
+  __syncthreads();
+  s.longest = max(max(sh.wave[0], sh.wave[1]), max(sh.wave[2], sh.wave[3]));
+  return s;
+}
 // Pages of a workgroup's run: an equal share of all items' pages, but not under an eighth of the mean item, up to 8.  A shorter run
 // costs more in its partial result (66 KB written and read for 128 columns of 128 channels, a page is 16 KB) than the others gain:
 // 128 tokens behind 4000 take 72 us in runs of 5 pages and 54 in runs of 9; where items are short themselves, 9 tokens behind
 // 100, runs of 8 pages take one workgroup through several items, 41 us for 25.
-__device__ __forceinline__ int64_t run_length(const AttnArgs &a, Shared &sh, int64_t &total) {
-  int64_t pages = 0, blocks = 0, all;
-  walk(a, sh, [&](const Place &p) {
-    pages += p.pages;
-    blocks += p.pages != 0;
-    return false;
-  });
-  (void)scan256(pages, sh.wave64, total);
-  (void)scan256(blocks, sh.wave64, all);
-  const int64_t least = min((int64_t)8, total / (8 * max(all, (int64_t)1)));
-  total *= a.c.heads;
-  return max(max((total + gridDim.x - 1) / gridDim.x, least), (int64_t)1);
+__device__ __forceinline__ int64_t run_length(const AttnArgs &a, const Sums &s) {
+  const int64_t least = min((int64_t)8, s.pages / (8 * max(s.blocks, 1)));
+  return max(max((s.pages * a.c.heads + a.groups - 1) / a.groups, least), (int64_t)1);
+}
+// Whether a workgroup had better take a whole item where there are fewer items than workgroups: a page takes some 1.3 us where
+// a CU has one workgroup and 2 where it has two; equal runs are shorter, but write and read their parts at some 3 TB/s and wait for
+// the joining.  (1024 tokens, us in runs : whole items, behind nothing 73 : 33, 4000 122 : 115, 30000 530 : 629.)
+template <int HD> __device__ __forceinline__ bool items_whole(const AttnArgs &a, const Sums &s, int64_t run) {
+  const float page1 = 1.3f * HD / 128, page2 = 2.0f * HD / 128;
+  const int cus = a.groups / (HD == 256 ? 1 : 2), items = s.blocks * a.c.heads;
+  const float runs = (float)((s.pages * a.c.heads + run - 1) / run), parts = fminf(runs + items, 2.0f * runs);
+  const float whole = s.longest * (items > cus ? page2 : page1);
+  const float shared = run * (runs > cus ? page2 : page1) + 8.0f + parts * (MANY * HD * 8) * (1.0f / 3e6f);
+  return whole <= shared;
 }
 
-// the block that holds unit `target`, and the unit's place in it: found[0], found[1], rest
+// the block that holds page `target` of all blocks' pages, and the page's place in it: found[0], found[1], rest
 __device__ __forceinline__ void find_unit(const AttnArgs &a, Shared &sh, int64_t target) {
   int64_t base = 0;
   if (threadIdx.x == 0) sh.found[0] = -1;
   walk(a, sh, [&](const Place &p) {
-    const int64_t units = (int64_t)p.pages * a.c.heads;
     int64_t total;
-    const int64_t at = base + scan256(units, sh.wave64, total) - units;
-    if (at <= target && target < at + units) {
+    const int64_t at = base + scan256((int64_t)p.pages, sh.wave64, total) - p.pages;
+    if (at <= target && target < at + p.pages) {
       sh.found[0] = p.b;
       sh.found[1] = p.j;
       sh.rest = target - at;
@@ -209,9 +235,9 @@ __device__ __forceinline__ void load_chunk(const AttnArgs &a, const Seq &s, int 
   amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
   int e = (int)(__float_as_uint(amax) >> 23) - 127 - 7;  // largest element to [2^7, 2^8)
   e = e < -118 ? -118 : e;
-  // a factor >= 0, so that the largest product is the largest score; not 0, which would make a number of a hidden one
+  // a factor >= 0, so that the largest product is the largest score
   const float down = __uint_as_float((uint32_t)(127 - e) << 23) * (a.scale < 0.0f ? -1.0f : 1.0f);
-  k.factor = fmaxf(ldexpf(fabsf(a.scale), e), 1e-37f);
+  k.factor = ldexpf(fabsf(a.scale), e);
   k.sight = valid ? sight_of(a, s, s.p0 + token) : Sight{-1, -1};
 #pragma unroll
   for (int i = 0; i < HD / 16; ++i) {
@@ -331,10 +357,10 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
       s[i >> 4][i & 15] = __uint_as_float((__float_as_uint(s[i >> 4][i & 15]) & m) | (0xff800000u & ~m));  // hidden: -infinity
     }
   }
-  const float factor = k.factor * kscale;
-  // a page of a smaller scale than the accumulators' unit: its weights are that much smaller, but not in the sum of weights
+  const float factor = fmaxf(k.factor * kscale, 1e-37f);  // not 0, which would make a number of a hidden score
+  // The accumulators' unit is a page's scale: a larger one takes over, and one that is smaller by more than 2^6, by at most 2^40 at a
+  // time.  A page of a smaller scale than the unit gets weights that are as much smaller, but not in the sum of weights.
   if (__builtin_amdgcn_readfirstlane((vscale > unit) | (vscale < unit * 0x1p-6f))) {
-    // a larger scale, or a much smaller one, becomes the unit (by at most 2^40 downwards at a time)
     const float low = unit * 0x1p-40f, to = uniform(vscale < low ? low : vscale), all = unit / to;
     unit = to;
 #pragma unroll
@@ -343,7 +369,8 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
       for (int r = 0; r < 16; ++r) k.acc[c][r] *= all;
   }
   float shift = CHUNK_BITS, count = 1.0f;
-  if (vscale != unit) {
+  const int tiny = vscale < unit * 0x1p-6f;  // (a page of zeros, say) such weights may be nothing in fp16: the sum is made without
+  if (vscale != unit && !tiny) {
     count = unit / vscale;
     shift -= __builtin_amdgcn_logf(count);
   }
@@ -365,7 +392,7 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
   };
   weigh(shift - k.m);
   // A weight beyond fp16 (infinity in the sum) asks for another reference: the maximum so far.
-  if (__builtin_amdgcn_readfirstlane(__ballot(sum == INFINITY) != 0)) {
+  if (__builtin_amdgcn_readfirstlane(__ballot(__float_as_uint(sum) == 0x7f800000u) != 0)) {
     float top = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
@@ -381,6 +408,7 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
     weigh(shift - k.m);
   }
   k.l += sum * count;
+  if (__builtin_amdgcn_readfirstlane(tiny)) weigh(CHUNK_BITS - __builtin_amdgcn_logf(unit / vscale) - k.m);
 #pragma unroll
   for (int c = 0; c < HD / 32; ++c) {
     u32x4(&x)[2] = v[EARLY ? c : 0];
@@ -425,7 +453,7 @@ __device__ __forceinline__ void settle_nan(const AttnArgs &a, Chunk<T, HD> &k, u
                                                    __builtin_bit_cast(f16x8, one), d, 0, 0, 0);
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) k.acc[c][r] = d[r] > 0.0f ? __uint_as_float(0x7fc00000u) : k.acc[c][r];
+      for (int r = 0; r < 16; ++r) k.acc[c][r] = __uint_as_float(d[r] > 0.0f ? 0x7fc00000u : __float_as_uint(k.acc[c][r]));
     }
   }
   __syncthreads();
@@ -440,17 +468,34 @@ __device__ __forceinline__ void settle_nan(const AttnArgs &a, Chunk<T, HD> &k, u
   __syncthreads();
 }
 
-// whole_items: a workgroup takes one item, the longest first (in the order of the blocks, three sequences of 2000 to 2500 tokens
-// behind 1000 to 3300 keep the chip busy for 237 pages' time, longest first 215, of 206 that all the work takes); else an equal run of the items' pages, as in the kernel for few columns.
+// ITEMS_WHOLE: a workgroup takes one item, the longest first (in the order of the blocks, three sequences of 2000 to 2500 tokens
+// behind 1000 to 3300 keep the chip busy for 237 pages' time, longest first 215, of 206 that all the work takes);
+// ITEMS_RUNS: an equal run of the items' pages, as in the kernel for few columns; ITEMS_EITHER: what the lengths say.
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_kernel(const AttnArgs a, int whole_items) {
+__global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_kernel(const AttnArgs a, ItemPlan items) {
   typedef Chunk<T, HD> C;
   __shared__ __align__(16) uint8_t tile[2][C::BYTES];
   __shared__ Shared sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
-  const int64_t w = blockIdx.x;
+  int64_t w = blockIdx.x;
   int b, head, j, x = 0;
   int64_t left, run = 1;
+  Sums sums = {0, 0, 0};
+  bool whole_items = items == ITEMS_WHOLE;
+  if (!whole_items) {
+    sums = sum_blocks(a, sh);
+    if (!sums.blocks) {
+      if (threadIdx.x == 0 && w < a.groups) a.header[w * 8 + H_PARTS] = 0;
+      return;
+    }
+    run = run_length(a, sums);
+    if (items == ITEMS_EITHER && items_whole<HD>(a, sums, run)) {
+      whole_items = true;
+      if (threadIdx.x == 0 && w < a.groups) a.header[w * 8 + H_PARTS] = 0;  // nothing to join
+    } else if (w >= a.groups) {
+      return;
+    }
+  }
   if (whole_items) {
     find_rank(a, sh, (int)(w / a.c.heads));
     if (sh.found[0] < 0) return;
@@ -459,19 +504,18 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
     head = (int)(w % a.c.heads);
     left = INT32_MAX;
   } else {
+    // Runs go through the blocks of one kv head after the other, and the workgroups of an XCD (every eighth) take neighbouring
+    // runs: what they read together is a head or two, and stays in their L2 (16384 tokens, 8 kv heads: 3.2 -> 2.2 ms).
+    const int64_t runs = (sums.pages * a.c.heads + run - 1) / run, eighth = (runs + 7) / 8;
+    w = w < 8 * eighth ? w % 8 * eighth + w / 8 : w;
     if (threadIdx.x == 0) a.header[w * 8 + H_PARTS] = 0;
-    int64_t total;
-    run = run_length(a, sh, total);
-    if (w * run >= total) return;
-    find_unit(a, sh, w * run);
+    if (w >= runs) return;
+    head = (int)(w * run / sums.pages);
+    find_unit(a, sh, w * run % sums.pages);
     b = sh.found[0];
     j = sh.found[1];
+    x = (int)sh.rest;
     left = run;
-    const Seq s = seq_of(a, b);
-    const Block k = block_of(a, s, j * MANY, MANY);
-    const int pages = span_of(a, s, k.first, k.last).pages;
-    head = (int)(sh.rest / pages);
-    x = (int)(sh.rest % pages);
   }
   b = __builtin_amdgcn_readfirstlane(b);
   head = __builtin_amdgcn_readfirstlane(head);
@@ -572,22 +616,23 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
     }
     at_start = false;
     if (whole_items || left <= 0) return;
-    // the next item: the next head, block, sequence with rows
+    // the next item: the next block, sequence with rows, head
     x = 0;
-    if (++head < a.c.heads) continue;
-    head = 0;
     if (++j < blocks_of(a, s.n, MANY)) continue;
     j = 0;
     do {
-      if (++b >= a.c.n_seqs) return;
+      if (++b >= a.c.n_seqs) {
+        b = 0;
+        if (++head >= a.c.heads) return;
+      }
     } while (rows_of(a.c, b).n == 0);
   }
 }
 
 }  // namespace
 
-void rvq_launch_cache8_chunk(const AttnArgs &a, bool half, int64_t groups, bool whole, hipStream_t s) {
-  const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * WAVES), 0, s, a, (int)whole); };
+void rvq_launch_cache8_chunk(const AttnArgs &a, bool half, int64_t grid, ItemPlan items, hipStream_t s) {
+  const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WAVES), 0, s, a, items); };
   if (a.c.hd == 64) half ? go(cache8_chunk_kernel<_Float16, 64>) : go(cache8_chunk_kernel<__bf16, 64>);
   else if (a.c.hd == 128) half ? go(cache8_chunk_kernel<_Float16, 128>) : go(cache8_chunk_kernel<__bf16, 128>);
   else half ? go(cache8_chunk_kernel<_Float16, 256>) : go(cache8_chunk_kernel<__bf16, 256>);

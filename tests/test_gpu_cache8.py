@@ -394,6 +394,22 @@ def test_attention_of_many_short_chunks(gpu_device, dtype):
     _attend_heads(case, dtype, 0.07, 0, 0, 2, 8, 64, (1,))
 
 
+@pytest.mark.parametrize("heads,hd,olds,news", [
+    (2, 128, [5], [300]), (2, 256, [0], [130]), (2, 64, [4000], [70]), (1, 256, [2500, 0, 60], [40, 0, 9]), (2, 128, [0, 3000], [500, 20])])
+def test_attention_of_a_few_chunks(gpu_device, heads, hd, olds, news):
+    """Fewer blocks of columns than workgroups: each a workgroup's own where all are short, shared where one is long."""
+    rng = np.random.default_rng(hd + len(news))
+    case = _attend_case(rng, "bf16", heads, 8, hd, olds, news)
+    _attend_heads(case, "bf16", 0.07, 0, 0, heads, 8, hd, (heads - 1,))
+
+
+def test_attention_of_more_than_a_thousand_chunks(gpu_device):
+    rng = np.random.default_rng(20)
+    news = [int(n) for n in rng.integers(0, 14, 1100)]
+    case = _attend_case(rng, "bf16", 1, 8, 64, [int(n) for n in rng.integers(0, 70, 1100)], news)
+    _attend_heads(case, "bf16", 0.07, 0, 0, 1, 8, 64, (0,))
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "fp16"])
 def test_sharp_and_flat_softmax(gpu_device, dtype):
     rng = np.random.default_rng(12)
@@ -415,6 +431,33 @@ def test_values_of_very_different_pages(gpu_device):
     scales[table[0, 4], 0, 0] = 2.0**-60
     got = _np(_attend(case, "fp32", 0.1))
     _check_attention(got, o.attend(codes, scales, q, cu, table, lengths, 0.1), "fp32", 64, 401, q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_chunks_over_values_of_very_different_pages(gpu_device, dtype):
+    """The same for many columns: pages of zeros that hold most of the weight, scales that jump up and down, in whole and in part."""
+    rng = np.random.default_rng(23)
+    for exps in ((-9, -100, -9, -100, -100, -8), (-100, -9, -30, 3, -9, -10), (-9, -11, -9, -13, -20, -60)):
+        case = _attend_case(rng, dtype, 1, 4, 64, [340], [40], sharp=0.1)
+        cu, table, lengths, codes, scales, q = case
+        for i, e in enumerate(exps):
+            scales[table[0, i], 0, 1] = 2.0**e
+            if e == -100:
+                codes[table[0, i], 0, 1] = 0
+        got = _np(_attend(case, dtype, 0.1))
+        # contributions of pages 2^-40 below another page's scale may be dropped: of 2^-40 of that page's values
+        _check_attention(got, o.attend(codes, scales, q, cu, table, lengths, 0.1), dtype, 64, 380, q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-30, 3.0])
+def test_chunks_with_softmax_scales_of_any_size_and_sign(gpu_device, dtype, scale):
+    rng = np.random.default_rng(24)
+    case = _attend_case(rng, dtype, 1, 4, 64, [100], [50], sharp=0.3)
+    cu, table, lengths, codes, scales, q = case
+    scales[:, :, 0] *= 2.0**-20 if scale == 0.0 else 1.0
+    got = _np(_attend(case, dtype, scale, 70, 3))
+    _check_attention(got, o.attend(codes, scales, q, cu, table, lengths, scale, 70, 3), dtype, 64, 150, q)
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
