@@ -236,7 +236,7 @@ int rvq_attn_decode(rvq_ctx *kctx, rvq_ctx *vctx, const float *dQ, int32_t n_q_h
  * the angle in 64 bits, rounded once (the angle of position p carries an error of about p 2^-52).
  *   dPositions  device, int64 [N]
  *   rot         even, >= 2
- *   base > 0, factor > 0, orig_len >= 0, amplitude finite; alpha < beta where orig_len > 0
+ *   base > 0, factor > 0, orig_len >= 0, amplitude finite in fp32; alpha < beta where orig_len > 0
  *   dCos, dSin  device, float [N][rot / 2]
  */
 int rvq_rope_tables(const int64_t *dPositions, int64_t N, int32_t rot, double base, double factor,
@@ -271,7 +271,7 @@ int rvq_rope(const void *dX, int32_t dtype, int64_t N, int32_t n_heads, int32_t 
  *   the values' codes  uint8 [head_dim][RVQ_PAGE_TOKENS]     (what a product of weights and values reads)
  * and, in an array of their own, the scales of the two.  A code is an e4m3 number (4 exponent and 3
  * mantissa bits, largest 448, no infinity, 0x7f / 0xff NaN), the value is code * scale.  A scale is a power of two:
- * it places the codes' range and costs them no precision.
+ * it places the codes' range and costs them no precision.  Caches that are filled in another way keep to that (2^-100 .. 2^120).
  * The struct is a host-side view; nothing is kept after a call.
  */
 #define RVQ_PAGE_TOKENS 64
@@ -303,6 +303,8 @@ typedef struct {
  *   dCos, dSin  device, float [rows][rot / 2], 16-byte aligned; both NULL (rot 0): keys are not rotated
  *   rot       a multiple of 16 up to head_dim
  * A page that the call writes must belong to one sequence (its one table entry), and no other call may use it at the same time.
+ * RVQ_EINVAL also where the pages that `rows` rows can span, times n_kv_heads, pass 2^31 - 1.  The stride of a single row or head
+ * does not matter.
  */
 int rvq_cache8_append(const rvq_cache8 *cache, const void *dK, const void *dV, int32_t dtype, int64_t rows,
                       int64_t ldk, int64_t hsk, int64_t ldv, int64_t hsv, const int32_t *dCu,
@@ -330,14 +332,18 @@ int rvq_cache8_read(const rvq_cache8 *cache, const int32_t *dCu, const int32_t *
  * (a sliding window, and a few first tokens that stay visible):
  *   out[a] = sum_t softmax_t(scale * q[a] . k[t, a / rep]) v[t, a / rep]
  * A row that sees nothing is 0.  What hidden and unwritten slots hold, NaN included, does not reach the result.
- * Scores, maxima, sums and weighted values are fp32; codes enter the matrix cores exactly, queries and weights as
- * fp16 (fp32 queries: two fp16 terms of each), see the kernel for the roundings.
+ * Scores, maxima, sums and weighted values are fp32; codes enter the matrix cores exactly.  Up to 32 columns a sequence (query
+ * tokens times rep, on the average), and with fp32 queries always, queries are fp16 scaled by a power of two per row (fp32: two
+ * such terms, 22 bits), weights fp16 (fp32 queries: two terms); with more columns queries are two (bf16) or three (fp16) e4m3 terms,
+ * which hold them as well, and weights fp16 with 11 bits down to 2^-16 of the largest at least.
  *   dQ      device, dtype [rows][n_q_heads][head_dim], 16-byte aligned, strides ldq, hsq in elements, multiples of
  *           16 bytes: already rotated
  *   dOut    the same with ldo, hso; dtype as dQ.  Must not overlap dQ.  Rows from cu[n_seqs] on are left as they were
- *   n_q_heads   a multiple of n_kv_heads
+ *   n_q_heads   a multiple of n_kv_heads, up to 65535; rows * rep up to 2^30 - 1
+ *   scale   finite, and so log2(e) scale in fp32
  *   dWorkspace  device, 16-byte aligned, workspace_bytes >= rvq_cache8_attn_workspace_bytes() of the same sizes on the
- *               current device; caller-owned, contents unspecified before and after
+ *               current device; caller-owned, contents unspecified before and after.  It serves one call at a time: calls
+ *               that may run side by side (streams, graphs) need one each
  * A table may name a page several times and share pages between sequences.
  * rvq_cache8_attn_workspace_bytes returns 0 for sizes that rvq_cache8_attn refuses.
  */

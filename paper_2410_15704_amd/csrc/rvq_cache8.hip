@@ -4,11 +4,17 @@
 // page and kv head, half of its threads the keys and half the values: it holds every token of a scale, so the scale
 // needs no second pass over memory and no atomics, and results do not depend on any order.  The pages of the step are
 // enumerated on the device (find_piece), since only the device knows the lengths; the grid is an upper bound.
+// Append of 16384 fp32 tokens of 32 kv heads of 128 channels: 153 us for 680 MB, 4.4 TB/s (a large copy 5.2: rows in, a quarter as many
+// bytes of codes out, and a barrier between); four bf16 chunks of up to 1500 tokens of 8 heads 10.9 us, single tokens of 32 sequences
+// 7.0.  Read of 131072 bf16 rows of 8 heads: 208 us for 872 MB, 4.2 TB/s (five bytes written and a table entry for one read); 48
+// rows 4.5 us.
 //
 // Keys are stored by token, values by channel (the order in which attention feeds both to the matrix cores
 // without a transposition).  A thread of the values takes four channels of 16 tokens: its reads and writes of rows are 8 or
 // 16 bytes, neighbours beside each other along the row, and of codes 16 bytes of a channel; what lies between is
 // a transposition of 4 x 4 bytes in registers (reading), or none (the conversion packs neighbouring tokens).
+// Through LDS instead: append of the chunks 16.4 us, read of the 131072 rows 231.
+// Appending takes 8 tokens a thread (16: chunks 12.3 us), reading 16.
 #include <type_traits>
 
 #include "rvq_cache8.h"

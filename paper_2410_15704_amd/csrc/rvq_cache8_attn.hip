@@ -1,4 +1,5 @@
-// Attention over the paged cache of 8-bit codes, for the query tokens of a step.
+// Attention over the paged cache of 8-bit codes, for the query tokens of a step: the kernel for few columns (single tokens), the
+// joining of partial results, the choice between this kernel and the one for many columns, and the entry point.
 //
 // Work.  The query heads that share a kv head, times the query tokens of a sequence, are columns; an item is a
 // block of columns of one (sequence, kv head), a unit one page of an item.  Units are numbered sequence by
@@ -24,12 +25,19 @@
 //
 // The scale of a page's keys enters the scores' factor.  Its values' scale becomes the unit of the accumulators,
 // which are multiplied by the powers of two between units along with the correction of the maximum.
+//
+// Bound by the codes' bytes: 131072 tokens of 8 kv heads of 128 channels are 268 MB, 51 us and 7 for the joining (5.3 TB/s; a large
+// copy moves 5.2); 64 sequences of 64 to 16000 tokens 195 + 5.4 us.  A short cache is bound by the chain of one run: 2100 tokens
+// take 12.1 us, of which some 7 go to finding the run, its table and the first page's way from memory, and 3.9 for the joining's launch.
+// Tried and taken back: the next page's codes in registers of their own (128 channels: spills, 131072 tokens 60 -> 84 us; 64 channels
+// 16.8 -> 17.5); three workgroups per CU for 64 channels (16.8 -> 16.9).
 #include <cmath>
 
 #include "rvq_cache8_attn.h"
 
 namespace {
 
+constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float WEIGHT_BITS = 14.0f;  // weights are held as 2^14 2^(s - m)
 
 // units (pages) of a sequence: as many for every block of its columns
@@ -540,8 +548,8 @@ Plan plan_of(int cus, int32_t dtype, int64_t rows, int n_seqs, int heads, int re
   Plan p;
   const int64_t seqs = rows < n_seqs ? rows : n_seqs, cols = rows * rep;
   p.many = dtype != RVQ_F32 && cols > 2 * COLS * seqs;
-  const int per_cu = p.many && hd == 256 ? 1 : 2;
-  p.groups = per_cu * cus < MOST_GROUPS ? per_cu * cus : MOST_GROUPS;
+  const int per_cu = p.many && hd == 256 ? 1 : 2, fit = per_cu * cus / 8 * 8;  // as many for every XCD
+  p.groups = fit < 8 ? 8 : fit < MOST_GROUPS ? fit : MOST_GROUPS;
   p.grid = p.groups;
   p.items = ITEMS_RUNS;
   const int64_t least = cols / MANY * heads, most = (cols / MANY + seqs) * heads;  // items
@@ -598,7 +606,7 @@ int64_t rvq_cache8_attn_workspace_bytes(const rvq_cache8 *cache, int32_t dtype, 
 int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int64_t rows, int32_t n_q_heads,
                     int64_t ldq, int64_t hsq, const int32_t *dCu, float scale, int32_t window, int32_t sinks,
                     void *dOut, int64_t ldo, int64_t hso, void *dWorkspace, int64_t workspace_bytes, void *stream) {
-  if (!attn_ok(cache, dtype, rows, n_q_heads) || !std::isfinite(scale) || window < 0 || sinks < 0) return RVQ_EINVAL;
+  if (!attn_ok(cache, dtype, rows, n_q_heads) || !std::isfinite(scale * LOG2E) || window < 0 || sinks < 0) return RVQ_EINVAL;
   if (rows == 0) return RVQ_OK;
   const int hd = cache->head_dim;
   if (!rvq_cache8_pointers_ok(cache) || !rvq_aligned(dCu, 4)) return RVQ_EINVAL;
@@ -616,7 +624,7 @@ int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int6
   a.ldq = ldq; a.hsq = hsq; a.ldo = ldo; a.hso = hso;
   a.rep = n_q_heads / cache->n_kv_heads;
   a.window = window; a.sinks = sinks;
-  a.scale = scale * 1.44269504088896340736f;
+  a.scale = scale * LOG2E;
   a.header = (int64_t *)dWorkspace;
   const Plan p = plan_of(cus, dtype, rows, cache->n_seqs, cache->n_kv_heads, a.rep, hd);
   a.groups = p.groups;

@@ -1,16 +1,24 @@
 // Attention over the paged cache of 8-bit codes for many columns (query tokens times the heads that share a kv head): chunks of prompts.
 //
-// The same arithmetic with 32x32x16 products: an item has 128 columns, 32 for each wavefront, and the four
+// The same arithmetic as for few columns, with 32x32 products: an item has 128 columns, 32 for each wavefront, and the four
 // share the page's 16 KiB of codes, which are copied to LDS a page ahead (straight from memory, 16 bytes a lane; pieces of
 // a row change places so that the wavefront's reads of neighbouring rows hit different banks).  A lane holds one
 // column and, of the two tiles of 32 tokens, the tokens 32 h .. 32 h + 31 (h = lane / 32): its weights are again what the
 // second product takes from it.
 //
-// The keys' codes go to the products as they are, against queries split into e4m3 terms.
-// What bounds it is the vector pipe: per page and wavefront 1024 clocks of matrix instructions stand against 64 conversions
-// and some 4 operations, one of them an exponential of four times the length, for each of a lane's 32 scores.  So the maximum that weights
-// refer to moves only when a score passes it by more than 2^7 (the accumulators are not touched otherwise), weights being
-// held as 2^8 2^(s - m) in fp16: at most 2^15, exact to 11 bits down to 2^-22 of the largest.
+// The keys' codes go to the products as they are, against queries split into e4m3 terms: two for bf16 (exact but for what lies
+// below 2^-21 of the row's largest element), three for fp16 (2^-25).  The values' codes become fp16, exactly, and so do the weights,
+// rounded to 11 bits.  The maximum that they refer to moves only where one passes fp16's range: weights are held as
+// 2^8 2^(s - m), so m may stay behind the true maximum by 2^7, and no maximum is taken per page, which would be two dependent
+// chains over 32 scores.  They keep 11 bits down to 2^-22 of the largest, or to 2^-16 where the scales of values differ between
+// pages (below).  The sum is of the rounded weights: their roundings cancel in a mean of equal values.
+//
+// What bounds it is issue: per page and wavefront (128 channels, bf16) 1024 clocks of matrix instructions stand against 64
+// conversions and some 4 operations, one of them an exponential of four times the length, for each of a lane's 32 scores; a probe
+// of the two kinds side by side takes the longer one's time and a third of the other's.  Three sequences of 2000 to 4096 tokens behind
+// up to 4000, 32 query heads on 8 kv heads of 128 channels: 435 us, 975 TFLOP/s, 81 % of what a large fp16 matrix product reaches.
+// Tried and taken back: the next page's scores between the exponentials (433 -> 458); s_setprio (no change); two pages to a
+// barrier (431 -> 457).
 
 #include "rvq_cache8_attn.h"
 
@@ -358,8 +366,8 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
     }
   }
   const float factor = fmaxf(k.factor * kscale, 1e-37f);  // not 0, which would make a number of a hidden score
-  // The accumulators' unit is a page's scale: a larger one takes over, and one that is smaller by more than 2^6, by at most 2^40 at a
-  // time.  A page of a smaller scale than the unit gets weights that are as much smaller, but not in the sum of weights.
+  // The accumulators' unit is a page's scale: a larger one takes over, and one that is smaller by more than 2^6 does, by at most 2^40
+  // at a time.  A page of a smaller scale than the unit gets weights that are as much smaller, but not in the sum of weights.
   if (__builtin_amdgcn_readfirstlane((vscale > unit) | (vscale < unit * 0x1p-6f))) {
     const float low = unit * 0x1p-40f, to = uniform(vscale < low ? low : vscale), all = unit / to;
     unit = to;

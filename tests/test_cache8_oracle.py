@@ -199,3 +199,8 @@ def test_the_binding_refuses_what_the_entry_points_cannot_see():
                  lambda: b.rope(q, torch.zeros(3, 32), torch.zeros(3, 32)), lambda: b.rope_tables(torch.zeros(3, dtype=torch.int64), 32)):
         with pytest.raises(ValueError):  # not on a GPU
             call()
+
+
+def test_numbers_that_pass_fp32_on_the_way_are_refused():
+    assert _attn(_view(), scale=3e38) == b.RVQ_EINVAL
+    assert b.lib.rvq_rope_tables(FAKE, 4, 32, 1e4, 1.0, 0.0, 1.0, 32.0, 1e300, FAKE, FAKE, None) == b.RVQ_EINVAL

@@ -9,6 +9,8 @@ Tolerances, all derived beforehand.
   attention  a score is off by E = scale sum |q| |k| times (2^-21 for two-term queries, 2^-22 of the row's largest element for the
              16-bit ones, and fp32 products and sums: head_dim + 8 roundings at most), a weight by the factor e^E, by 2^-11
              where it is rounded to fp16 (2^-21 with fp32 queries) and 2^-22 from exp2; sums over N tokens add (N / 32 + 48) 2^-23.
+             (Many columns take queries as e4m3 terms of 4 bits, two for bf16 and three for fp16: exact but for elements below 2^-14 of
+             the row's largest, those to 2^-21 and 2^-25 of it; no more is allowed for that.)
              All of it acts on sum w |v|; then half a step of the type."""
 import numpy as np
 import pytest
