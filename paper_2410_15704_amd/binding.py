@@ -542,7 +542,8 @@ class Cache8:
             raise ValueError(f"out: {q.dtype} expected, got {out.dtype}")
         po, ldo, hso = _heads(out, "out", heads, hd, dev, rows)
         if workspace is None:
-            workspace = torch.empty(self.workspace_bytes(q, view.n_seqs), dtype=torch.uint8, device=dev)
+            size = _at(dev, lib.rvq_cache8_attn_workspace_bytes, view, dtype, rows, heads)
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
         pw = _whole(workspace, "workspace", torch.uint8, workspace.shape, dev)
         _run(dev, lib.rvq_cache8_attn, view, pq, dtype, rows, heads, ldq, hsq, pcu, scale if scale is not None else hd**-0.5,
              window, sinks, po, ldo, hso, pw, workspace.numel())

@@ -18,7 +18,8 @@
 // of the two kinds side by side takes the longer one's time and a third of the other's.  Three sequences of 2000 to 4096 tokens behind
 // up to 4000, 32 query heads on 8 kv heads of 128 channels: 435 us, 975 TFLOP/s, 81 % of what a large fp16 matrix product reaches.
 // Tried and taken back: the next page's scores between the exponentials (433 -> 458); s_setprio (no change); two pages to a
-// barrier (431 -> 457).
+// barrier (431 -> 457); values turned into fp16 by one wavefront for all four, through LDS: a fifth fewer vector instructions and
+// twice the reads of LDS (435 -> 475).
 
 #include "rvq_cache8_attn.h"
 
