@@ -16,7 +16,6 @@ namespace {
 
 constexpr int PAGE = RVQ_PAGE_TOKENS;
 
-
 // rows of sequence b in this step; whatever the array holds, they lie inside [0, rows)
 struct SeqRows {
   int64_t row;
@@ -66,6 +65,55 @@ __device__ __forceinline__ bool find_piece(int n_seqs, N at, Count count, int &s
       return true;
     }
     before += __shfl(sum, 63, 64);
+  }
+  return false;
+}
+
+// The same by the whole workgroup, THREADS sequences per trip, for more than 64 sequences: a trip is a chain of loads (cu, lengths),
+// and it is these chains, not the additions, that many sequences cost.  For 64 and less the barriers are saved.
+template <int THREADS, typename N> struct Together {
+  N sums[THREADS / 64], inside;
+  int seq;
+};
+// Inclusive prefix sum over the workgroup's threads, and the sum of all.  Ends behind a barrier; another one has to come before
+// the next call.
+template <int THREADS, typename N> __device__ __forceinline__ N scan_all(N x, Together<THREADS, N> &sh, N &total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const N o = __shfl_up(x, d, 64);
+    if (lane >= d) x += o;
+  }
+  if (lane == 63) sh.sums[wave] = x;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    const N s = sh.sums[w];
+    if (w < wave) x += s;
+    total += s;
+  }
+  return x;
+}
+template <int THREADS, typename N, typename Count>
+__device__ __forceinline__ bool find_piece_together(int n_seqs, N at, Count count, Together<THREADS, N> &sh, int &seq, N &inside) {
+  N before = 0;
+  for (int b0 = 0; b0 < n_seqs; b0 += THREADS) {
+    const int b = b0 + (int)threadIdx.x;
+    const N c = b < n_seqs ? count(b) : 0;
+    N total;
+    const N upto = before + scan_all<THREADS, N>(c, sh, total);
+    if (upto > at && upto - c <= at) {
+      sh.seq = b;
+      sh.inside = at - (upto - c);
+    }
+    __syncthreads();
+    before += total;
+    if (before > at) {  // the same in every thread
+      seq = sh.seq;
+      inside = sh.inside;
+      return true;
+    }
   }
   return false;
 }

@@ -40,14 +40,18 @@ struct Span {
   int lo, hi;          // slots of the page that the step's rows fill
 };
 
-template <bool READ> __device__ __forceinline__ bool find_span(const MoveArgs &a, Span &s) {
+template <bool READ, int THREADS> __device__ __forceinline__ bool find_span(const MoveArgs &a, Span &s) {
+  __shared__ Together<THREADS, int> sh;
   int inside;
   const auto first_position = [&](int b, int n) -> int64_t { return READ ? a.first[b] : (int64_t)a.c.lengths[b] - n; };
   const auto count = [&](int b) -> int {
     const SeqRows r = rows_of(a.c, b);
     return r.n ? (int)pages_spanned(first_position(b, r.n), r.n) : 0;
   };
-  if (!find_piece<int>(a.c.n_seqs, blockIdx.x / a.c.heads, count, s.b, inside)) return false;
+  const int at = blockIdx.x / a.c.heads;
+  if (!(a.c.n_seqs <= 64 ? find_piece<int>(a.c.n_seqs, at, count, s.b, inside)
+                         : find_piece_together<THREADS, int>(a.c.n_seqs, at, count, sh, s.b, inside)))
+    return false;
   const SeqRows r = rows_of(a.c, s.b);
   s.n = r.n;
   s.row = r.row;
@@ -97,7 +101,7 @@ template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(4 * HD) v
   constexpr int TOK = 8, KEYS = TOK / 4, WAVES_HALF = Task<HD, TOK>::HALF / 64;
   __shared__ uint32_t wave_max[2 * WAVES_HALF];
   Span s;
-  if (!find_span<false>(a, s) || s.page < 0) return;
+  if (!find_span<false, 4 * HD>(a, s) || s.page < 0) return;
   const int head = blockIdx.x % a.c.heads;
   const Task<HD, TOK> task;
   float *scale_at = scale_of(a.c, s.page, head, task.values);
@@ -254,7 +258,7 @@ template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(4 * HD) v
 
 template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) void cache8_read_kernel(const MoveArgs a) {
   Span s;
-  if (!find_span<true>(a, s)) return;
+  if (!find_span<true, 2 * HD>(a, s)) return;
   const int head = blockIdx.x % a.c.heads;
   const Task<HD, 16> task;
   T *dst = (T *)(task.values ? a.v : a.k);

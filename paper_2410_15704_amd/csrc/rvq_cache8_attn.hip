@@ -46,9 +46,10 @@ __device__ __forceinline__ int64_t units_of(const AttnArgs &a, int b) {
   return (int64_t)blocks_of(a, s.n, COLS) * a.c.heads * span_of(a, s, s.p0, s.p0 + s.n - 1).pages;
 }
 
-// The run of workgroup `w`: how many units a run has, and the sequence and place of its first one.  Every wavefront computes it.
-// Up to 64 sequences are a lane each, and one prefix sum gives both.
+// The run of workgroup `w`: how many units a run has, and the sequence and place of its first one.  Every wavefront computes it
+// for up to 64 sequences, a lane each, and one prefix sum gives both; more are taken by the workgroup together.
 __device__ __forceinline__ bool find_run(const AttnArgs &a, int64_t w, int64_t &run, int &seq, int64_t &inside) {
+  __shared__ Together<64 * WAVES, int64_t> sh;
   const int lane = threadIdx.x & 63;
   const auto run_of = [&](int64_t total) {
     const int64_t even = (total + gridDim.x - 1) / gridDim.x;
@@ -73,12 +74,12 @@ __device__ __forceinline__ bool find_run(const AttnArgs &a, int64_t w, int64_t &
       return true;
     }
   }
-  int64_t total = 0;
-  for (int b = lane; b < a.c.n_seqs; b += 64) total += units_of(a, b);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d, 64);
+  int64_t mine = 0, total;
+  for (int b = threadIdx.x; b < a.c.n_seqs; b += 64 * WAVES) mine += units_of(a, b);
+  (void)scan_all<64 * WAVES, int64_t>(mine, sh, total);
+  __syncthreads();
   run = run_of(total);
-  return find_piece<int64_t>(a.c.n_seqs, w * run, [&](int i) { return units_of(a, i); }, seq, inside);
+  return find_piece_together<64 * WAVES, int64_t>(a.c.n_seqs, w * run, [&](int i) { return units_of(a, i); }, sh, seq, inside);
 }
 
 template <typename T, int HD> struct Columns {
