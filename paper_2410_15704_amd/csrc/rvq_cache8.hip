@@ -5,9 +5,9 @@
 // needs no second pass over memory and no atomics, and results do not depend on any order.  The pages of the step are
 // enumerated on the device (find_piece), since only the device knows the lengths; the grid is an upper bound.
 // Append of 16384 fp32 tokens of 32 kv heads of 128 channels: 153 us for 680 MB, 4.4 TB/s (a large copy 5.2: rows in, a quarter as many
-// bytes of codes out, and a barrier between); four bf16 chunks of up to 1500 tokens of 8 heads 10.9 us, single tokens of 32 sequences
-// 7.0.  Read of 131072 bf16 rows of 8 heads: 208 us for 872 MB, 4.2 TB/s (five bytes written and a table entry for one read); 48
-// rows 4.5 us.
+// bytes of codes out, and a barrier between); four fp16 chunks of up to 1500 tokens of 8 heads 10.9 us, single tokens of 32 sequences
+// 5.0 (by the kernel for a few tokens).  Read of 131072 fp16 rows of 8 heads: 208 us for 872 MB, 4.2 TB/s (two bytes written for one
+// read, and a table entry per pair); 48 rows 4.9 us.
 //
 // Keys are stored by token, values by channel (the order in which attention feeds both to the matrix cores
 // without a transposition).  A thread of the values takes four channels of 16 tokens: its reads and writes of rows are 8 or
@@ -40,15 +40,15 @@ struct Span {
   int lo, hi;          // slots of the page that the step's rows fill
 };
 
-template <bool READ, int THREADS> __device__ __forceinline__ bool find_span(const MoveArgs &a, Span &s) {
+// the step's page `at`
+template <bool BACK, int THREADS> __device__ __forceinline__ bool find_span(const MoveArgs &a, int at, Span &s) {
   __shared__ Together<THREADS, int> sh;
   int inside;
-  const auto first_position = [&](int b, int n) -> int64_t { return READ ? a.first[b] : (int64_t)a.c.lengths[b] - n; };
+  const auto first_position = [&](int b, int n) -> int64_t { return BACK ? a.first[b] : (int64_t)a.c.lengths[b] - n; };
   const auto count = [&](int b) -> int {
     const SeqRows r = rows_of(a.c, b);
     return r.n ? (int)pages_spanned(first_position(b, r.n), r.n) : 0;
   };
-  const int at = blockIdx.x / a.c.heads;
   if (!(a.c.n_seqs <= 64 ? find_piece<int>(a.c.n_seqs, at, count, s.b, inside)
                          : find_piece_together<THREADS, int>(a.c.n_seqs, at, count, sh, s.b, inside)))
     return false;
@@ -101,7 +101,7 @@ template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(4 * HD) v
   constexpr int TOK = 8, KEYS = TOK / 4, WAVES_HALF = Task<HD, TOK>::HALF / 64;
   __shared__ uint32_t wave_max[2 * WAVES_HALF];
   Span s;
-  if (!find_span<false, 4 * HD>(a, s) || s.page < 0) return;
+  if (!find_span<false, 4 * HD>(a, blockIdx.x / a.c.heads, s) || s.page < 0) return;
   const int head = blockIdx.x % a.c.heads;
   const Task<HD, TOK> task;
   float *scale_at = scale_of(a.c, s.page, head, task.values);
@@ -256,9 +256,120 @@ template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(4 * HD) v
   }
 }
 
+// Append where sequences bring a token or a few: the same results by a wavefront per (page, head, keys or values), four of them a
+// workgroup.  It is a chain of latencies (lengths, table, rows and old scale, codes), so what counts is how many of them a CU holds:
+// 20 scales at a time instead of 4.  A lane takes neighbouring channels, N tokens at a time with all loads before the first product (8
+// tokens: 512 sequences 13.3 -> 15.7 us, fewer wavefronts fit); a page of more tokens than N is read twice.
+template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(256) void cache8_append_few_kernel(const MoveArgs a) {
+  constexpr int C = HD / 64, N = HD == 256 ? 2 : 4;
+  const int pairs = (a.c.heads + 1) / 2, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Span s;
+  if (!find_span<false, 256>(a, blockIdx.x / pairs, s) || s.page < 0) return;
+  const int head = (int)(blockIdx.x % pairs) * 2 + (wave >> 1);
+  const bool values = wave & 1;
+  if (head >= a.c.heads) return;
+  float *scale_at = scale_of(a.c, s.page, head, values);
+  const float old = s.lo ? *scale_at : 0.0f;
+  uint8_t *codes = codes_of(a.c, s.page, head, values);
+  const T *src = values ? (const T *)a.v + head * a.hsv : (const T *)a.k + head * a.hsk;
+  const int64_t ld = values ? a.ldv : a.ldk;
+  const int half = values ? 0 : a.rot / 2;
+  // the channel that each of the lane's is turned with (itself: none) and the pair's entry of the tables
+  int partner[C], pair[C];
+  bool first[C];
+#pragma unroll
+  for (int j = 0; j < C; ++j) {
+    const int c = lane * C + j;
+    first[j] = LAYOUT == RVQ_ROPE_HALVES ? c < half : !(c & 1);
+    partner[j] = c >= 2 * half ? c : LAYOUT == RVQ_ROPE_HALVES ? (first[j] ? c + half : c - half) : c ^ 1;
+    pair[j] = c >= 2 * half ? 0 : LAYOUT == RVQ_ROPE_HALVES ? min(c, partner[j]) : c >> 1;
+  }
+  float x[N][C], top = 0.0f;
+  const auto load = [&](int slot0) {  // N tokens from slot0 on, and their largest magnitude
+    typedef T Own __attribute__((ext_vector_type(C)));
+    Own own[N];
+    T other[N][C];
+    float cs[N][C], sn[N][C];
+#pragma unroll
+    for (int i = 0; i < N; ++i) own[i] = *reinterpret_cast<const Own *>(src + row_of(s, nearest(s, slot0 + i)) * ld + lane * C);
+    if (half) {  // all loads before the first product
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+          const int64_t row = row_of(s, nearest(s, slot0 + i));
+          other[i][j] = src[row * ld + partner[j]];
+          cs[i][j] = a.cos[row * half + pair[j]];
+          sn[i][j] = a.sin[row * half + pair[j]];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < C; ++j) x[i][j] = (float)own[i][j];
+    if (half) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+          const float y = (float)other[i][j];
+          float u = first[j] ? x[i][j] : y, v = first[j] ? y : x[i][j];
+          rotate_pair(u, v, cs[i][j], sn[i][j]);
+          x[i][j] = partner[j] == lane * C + j ? x[i][j] : first[j] ? u : v;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < C; ++j) top = not_finite(x[i][j]) ? top : fmaxf(top, fabsf(x[i][j]));
+  };
+  for (int slot0 = s.lo; slot0 < s.hi; slot0 += N) load(slot0);
+#pragma unroll
+  for (int d = 32; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+  float scale = code_scale(top);
+  scale = s.lo ? fmaxf(scale, old) : scale;
+  const float inverse = 1.0f / scale;
+  if (lane == 0) *scale_at = scale;
+  if (s.lo && scale > old) {  // the page's earlier tokens
+    const float ratio = old * inverse;
+    const int pieces = values ? HD * PAGE / 16 : s.lo * HD / 16;
+    for (int i = lane; i < pieces; i += 64) {
+      const int first = values ? i % (PAGE / 16) * 16 : 0, held = values ? s.lo - first : 16;  // bytes of the piece that change
+      if (held <= 0) continue;
+      u32x4 v = *reinterpret_cast<const u32x4 *>(codes + i * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int n = held - 4 * j;
+        const uint32_t mask = n <= 0 ? 0u : n >= 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
+        v[j] = (again4(v[j], ratio) & mask) | (v[j] & ~mask);
+      }
+      *reinterpret_cast<u32x4 *>(codes + i * 16) = v;
+    }
+    __threadfence_block();  // some of these bytes are written once more below, by other lanes
+  }
+  for (int slot0 = s.lo; slot0 < s.hi; slot0 += N) {
+    if (s.hi - s.lo > N) load(slot0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (slot0 + i >= s.hi) break;
+      float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < C; ++j) y[j] = x[i][j] * inverse;
+      const uint32_t w = encode4_any(y[0], y[1], y[2], y[3]);
+      if (values) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) codes[(lane * C + j) * PAGE + slot0 + i] = (uint8_t)(w >> (8 * j));
+      } else {
+        typedef std::conditional_t<C == 1, uint8_t, std::conditional_t<C == 2, uint16_t, uint32_t>> Word;
+        *reinterpret_cast<Word *>(codes + (slot0 + i) * HD + lane * C) = (Word)w;
+      }
+    }
+  }
+}
+
 template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) void cache8_read_kernel(const MoveArgs a) {
   Span s;
-  if (!find_span<true, 2 * HD>(a, s)) return;
+  if (!find_span<true, 2 * HD>(a, blockIdx.x / a.c.heads, s)) return;
   const int head = blockIdx.x % a.c.heads;
   const Task<HD, 16> task;
   T *dst = (T *)(task.values ? a.v : a.k);
@@ -347,28 +458,29 @@ int64_t most_pages(int64_t rows, int n_seqs) {
   return most < rows ? most : rows;
 }
 
-template <bool READ, typename T, int HD> void launch_move(const MoveArgs &a, int layout, dim3 grid, hipStream_t s) {
-  if (layout == RVQ_ROPE_HALVES) {
-    if (READ) hipLaunchKernelGGL((cache8_read_kernel<T, HD, RVQ_ROPE_HALVES>), grid, dim3(2 * HD), 0, s, a);
-    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_HALVES>), grid, dim3(4 * HD), 0, s, a);
-  } else {
-    if (READ) hipLaunchKernelGGL((cache8_read_kernel<T, HD, RVQ_ROPE_ADJACENT>), grid, dim3(2 * HD), 0, s, a);
-    else hipLaunchKernelGGL((cache8_append_kernel<T, HD, RVQ_ROPE_ADJACENT>), grid, dim3(4 * HD), 0, s, a);
-  }
+enum Move { READ, APPEND, APPEND_FEW };
+template <Move WHAT, typename T, int HD, int LAYOUT> void launch_move(const MoveArgs &a, dim3 grid, hipStream_t s) {
+  if constexpr (WHAT == READ) hipLaunchKernelGGL((cache8_read_kernel<T, HD, LAYOUT>), grid, dim3(2 * HD), 0, s, a);
+  else if constexpr (WHAT == APPEND) hipLaunchKernelGGL((cache8_append_kernel<T, HD, LAYOUT>), grid, dim3(4 * HD), 0, s, a);
+  else hipLaunchKernelGGL((cache8_append_few_kernel<T, HD, LAYOUT>), grid, dim3(256), 0, s, a);
 }
-template <bool READ, typename T> void launch_move_hd(const MoveArgs &a, int layout, dim3 grid, hipStream_t s) {
-  if (a.c.hd == 64) launch_move<READ, T, 64>(a, layout, grid, s);
-  else if (a.c.hd == 128) launch_move<READ, T, 128>(a, layout, grid, s);
-  else launch_move<READ, T, 256>(a, layout, grid, s);
+template <Move WHAT, typename T, int HD> void launch_move_layout(const MoveArgs &a, int layout, dim3 grid, hipStream_t s) {
+  if (layout == RVQ_ROPE_HALVES) launch_move<WHAT, T, HD, RVQ_ROPE_HALVES>(a, grid, s);
+  else launch_move<WHAT, T, HD, RVQ_ROPE_ADJACENT>(a, grid, s);
 }
-template <bool READ> int move(const MoveArgs &a, int layout, int32_t dtype, hipStream_t s) {
+template <Move WHAT, typename T> void launch_move_hd(const MoveArgs &a, int layout, dim3 grid, hipStream_t s) {
+  if (a.c.hd == 64) launch_move_layout<WHAT, T, 64>(a, layout, grid, s);
+  else if (a.c.hd == 128) launch_move_layout<WHAT, T, 128>(a, layout, grid, s);
+  else launch_move_layout<WHAT, T, 256>(a, layout, grid, s);
+}
+template <Move WHAT> int move(const MoveArgs &a, int layout, int32_t dtype, hipStream_t s) {
   // the heads of a page beside each other: their rows are neighbours in memory, and they read the same tables
   const int64_t blocks = most_pages(a.c.rows, a.c.n_seqs) * a.c.heads;
   if (blocks > INT32_MAX) return RVQ_EINVAL;
-  const dim3 grid((unsigned)blocks);
-  if (dtype == RVQ_F32) launch_move_hd<READ, float>(a, layout, grid, s);
-  else if (dtype == RVQ_BF16) launch_move_hd<READ, __bf16>(a, layout, grid, s);
-  else launch_move_hd<READ, _Float16>(a, layout, grid, s);
+  const dim3 grid((unsigned)(WHAT == APPEND_FEW ? blocks / a.c.heads * ((a.c.heads + 1) / 2) : blocks));
+  if (dtype == RVQ_F32) launch_move_hd<WHAT, float>(a, layout, grid, s);
+  else if (dtype == RVQ_BF16) launch_move_hd<WHAT, __bf16>(a, layout, grid, s);
+  else launch_move_hd<WHAT, _Float16>(a, layout, grid, s);
   return hipGetLastError() == hipSuccess ? RVQ_OK : RVQ_EHIP;
 }
 
@@ -397,7 +509,11 @@ int rvq_cache8_append(const rvq_cache8 *cache, const void *dK, const void *dV, i
   if (!rvq_rows16_ok(dK, dtype, rows, heads, hd, ldk, hsk) || !rvq_rows16_ok(dV, dtype, rows, heads, hd, ldv, hsv)) return RVQ_EINVAL;
   if (!rvq_stream_is_current((hipStream_t)stream)) return RVQ_EINVAL;
   MoveArgs a = {view_of(cache, dCu, rows), nullptr, (char *)dK, (char *)dV, ldk, hsk, ldv, hsv, dCos, dSin, rot};
-  return move<false>(a, layout, dtype, (hipStream_t)stream);
+  // Up to 512 channels of new tokens a sequence, on the average: a wavefront a scale (us, a workgroup a scale : a wavefront; 8 heads
+  // of 128 channels, 32 sequences, a token each 5.8 : 4.5, 512 sequences 43 : 13, of 4 tokens 56 : 21, of 8 62 : 34, but 4 sequences of
+  // 8 tokens 5.8 : 6.8 and 64 of 16 11 : 15; 500 single tokens beside a chunk of 1500 53 : 38).
+  if (rows * hd <= 512 * (int64_t)cache->n_seqs) return move<APPEND_FEW>(a, layout, dtype, (hipStream_t)stream);
+  return move<APPEND>(a, layout, dtype, (hipStream_t)stream);
 }
 
 int rvq_cache8_read(const rvq_cache8 *cache, const int32_t *dCu, const int32_t *dFirst, int64_t rows,
@@ -411,7 +527,7 @@ int rvq_cache8_read(const rvq_cache8 *cache, const int32_t *dCu, const int32_t *
   if (dV && (!rvq_rows16_ok(dV, dtype, rows, heads, hd, ldv, hsv) || !rvq_rows_distinct(rows, heads, hd, ldv, hsv))) return RVQ_EINVAL;
   if (!rvq_stream_is_current((hipStream_t)stream)) return RVQ_EINVAL;
   MoveArgs a = {view_of(cache, dCu, rows), dFirst, (char *)dK, (char *)dV, ldk, hsk, ldv, hsv, dCos, dSin, rot};
-  return move<true>(a, layout, dtype, (hipStream_t)stream);
+  return move<READ>(a, layout, dtype, (hipStream_t)stream);
 }
 
 }  // extern "C"

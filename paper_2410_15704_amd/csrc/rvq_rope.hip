@@ -1,7 +1,7 @@
 // Rotary position tables, and the rotation of head vectors (queries).
 //
 // Both are bound by memory: a table entry costs an fp64 angle once per step, the rotation three
-// operations per element that is read and written once.  16384 tokens of 32 heads of 128 channels, 64 of them rotated, bf16,
+// operations per element that is read and written once.  16384 tokens of 32 heads of 128 channels, 64 of them rotated, fp16,
 // tables included: 58 us for 273 MB, 4.7 TB/s of the 5.2 that a large copy reaches.  64 tokens: 3.1 us for the tables, 3.2 for the
 // rotation, which are launches.  Stores past the caches would gain some (58 -> 55 us) and cost the next call, which reads these rows.
 #include <algorithm>

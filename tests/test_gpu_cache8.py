@@ -506,6 +506,49 @@ def test_rows_that_see_nothing_are_zero_and_missing_pages_are_not_seen(gpu_devic
         _check_attention(got, want, "bf16", 64, int(lengths.max()), q)
 
 
+def _among_empty(cu, table, lengths, front, back, rng):
+    """The same step with sequences that bring nothing before and behind."""
+    def around(x, a, z):
+        return np.concatenate([a, x, z]).astype(np.int32)
+
+    n = table.shape[1]
+    some = lambda k: rng.integers(-5, 300, k)  # noqa: E731
+    return (around(cu, np.zeros(front), np.full(back, cu[-1])), around(table, rng.integers(-3, 9, (front, n)), rng.integers(-3, 9, (back, n))),
+            around(lengths, some(front), some(back)))
+
+
+@pytest.mark.parametrize("front,back", [(3, 61), (70, 30), (400, 1100)])
+@pytest.mark.parametrize("dtype,heads,hd,rot,layout", [("bf16", 3, 64, 32, o.HALVES), ("fp16", 2, 128, 128, o.ADJACENT), ("fp32", 1, 128, 64, o.HALVES),
+                                                       ("bf16", 3, 256, 256, o.ADJACENT), ("fp16", 1, 256, 0, o.HALVES), ("fp32", 2, 64, 64, o.ADJACENT)])
+def test_sequences_that_bring_nothing_change_nothing(gpu_device, front, back, dtype, heads, hd, rot, layout):
+    """Bit for bit, though other kernels and other searches run: append, read and attention of single tokens."""
+    torch, b, rng = _t(), _b(), np.random.default_rng(front + hd)
+    olds, news = [0, 5, 63, 100, 64, 20, 33], [1, 60, 1, 3, 70, 1, 9]
+    cu, table, lengths, codes, scales, k, v, cos, sin = _append_case(rng, dtype, heads, hd, rot, layout, olds, news, big=30.0, extra_rows=1)
+    k[0, 0, 5], k[2, -1, 0], v[1, 0, 3] = np.nan, np.inf, -np.inf
+    want = o.append(codes, scales, k, v, cu, table, lengths, None if cos is None else cos.astype(np.float64),
+                    None if sin is None else sin.astype(np.float64), layout)
+    kw = dict(cos=None if cos is None else _dev(cos), sin=None if sin is None else _dev(sin), layout=layout)
+    rows, first = k.shape[0], np.maximum(lengths - 20, 0).astype(np.int32)
+    wide = _among_empty(cu, table, lengths, front, back, rng)
+    results = []
+    for arrays, f in (((cu, table, lengths), first), (wide, np.concatenate([np.zeros(front), first, np.zeros(back)]))):
+        cache = b.Cache8(_dev(codes), _dev(scales.astype(np.float32)))
+        args = tuple(_i32(x) for x in arrays)
+        cache.append(_dev(k, _type(dtype)), _dev(v, _type(dtype)), *args, **kw)
+        out = tuple(torch.zeros(rows, heads, hd, device="cuda", dtype=_type(dtype)) for _ in range(2))
+        cache.read(rows, args[0], _i32(f), *args[1:], out=out, **kw)
+        results.append((cache.pages, cache.scales, *(x.view(torch.int32 if dtype == "fp32" else torch.int16) for x in out)))
+    for one, other in zip(*results):
+        assert torch.equal(one, other)
+    _check_append(results[1][0].cpu().numpy(), _np(results[1][1]), want, codes, (cu, table, lengths, codes, scales, k, v, cos, sin))
+    case = _attend_case(rng, dtype, heads, 4, hd, [0, 5, 63, 100, 64, 2000, 33] * 3, [1, 1, 0, 1, 1, 1, 1] * 3)
+    cu, table, lengths, codes, scales, q = case
+    got = _attend(case, dtype, 0.1)
+    wide = _among_empty(cu, table, lengths, front, back, rng)
+    assert torch.equal(got, _attend((*wide, codes, scales, q), dtype, 0.1))
+
+
 def test_step_arrays_that_make_no_sense_stay_in_bounds(gpu_device):
     """cu beyond the rows, descending, negative: rows are clamped to the step's, no row is read or written outside."""
     torch, b, rng = _t(), _b(), np.random.default_rng(16)
