@@ -317,7 +317,7 @@ __device__ __forceinline__ Range range_of(const AttnArgs &a, const Seq &s, const
   const int seen = min(k.last, s.tokens - 1), seen_by_all = min(k.first, s.tokens - 1);
   Range r;
   r.from = a.sinks > span.begin * PAGE ? span.sink_pages : max(span.sink_pages, (hide + 1) / PAGE + shift);
-  r.to = (seen < 0 ? 0 : seen / PAGE + 1) + shift;
+  r.to = max(span.sink_pages, (seen < 0 ? 0 : seen / PAGE + 1) + shift);  // (less: a window that begins behind the table's end)
   r.all_from = max(span.sink_pages, (hide_all + PAGE) / PAGE + shift);
   r.all_to = (seen_by_all + 1) / PAGE + shift;
   return r;

@@ -742,6 +742,94 @@ def test_results_do_not_depend_on_the_run(gpu_device):
         assert torch.equal(_attend(case, "bf16", 0.05), first)
 
 
+@pytest.mark.parametrize("dtype,rep", [("fp32", 2), ("bf16", 2), ("fp16", 60)])
+def test_windows_and_sinks_of_the_largest_sizes(gpu_device, dtype, rep):
+    """Beyond every length, alone and together, they hide nothing; a window of the length and no sinks likewise."""
+    rng, most = np.random.default_rng(60), 2**31 - 1
+    case = _attend_case(rng, dtype, 1, rep, 64, [300, 0, 70], [3, 1, 1])
+    cu, table, lengths, codes, scales, q = case
+    full = _np(_attend(case, dtype, 0.1))
+    _check_attention(full, o.attend(codes, scales, q, cu, table, lengths, 0.1), dtype, 64, 303, q)
+    for window, sinks in ((most, 0), (most, most), (1, most), (303, 0), (0, most)):
+        want = o.attend(codes, scales, q, cu, table, lengths, 0.1, window, sinks)
+        _check_attention(_np(_attend(case, dtype, 0.1, window=window, sinks=sinks)), want, dtype, 64, 303, q)
+        assert np.allclose(want[0], o.attend(codes, scales, q, cu, table, lengths, 0.1)[0], atol=1e-12)
+
+
+@pytest.mark.parametrize("dtype,rep", [("fp32", 1), ("bf16", 3), ("bf16", 50), ("fp16", 40)])
+def test_tokens_behind_the_table_and_shared_pages(gpu_device, dtype, rep):
+    """Lengths beyond the table's room: queries out there see what the table holds.  Pages named twice and by two sequences."""
+    rng = np.random.default_rng(61)
+    case = _attend_case(rng, dtype, 2, rep, 128, [100, 190, 64, 200], [2, 1, 3, 4])
+    cu, table, lengths, codes, scales, q = case
+    table[0, :2] = table[1, [2, 2]]
+    table[2, :2] = table[1, :2]
+    lengths = lengths.copy()
+    lengths[1] = 64 * table.shape[1] + 1000   # its query has no page
+    lengths[3] = 64 * table.shape[1] + 2      # two of its queries have none
+    case = cu, table, lengths, codes, scales, q
+    for window, sinks in ((0, 0), (90, 3), (5, 0)):
+        want = o.attend(codes, scales, q, cu, table, lengths, 0.06, window, sinks)
+        _check_attention(_np(_attend(case, dtype, 0.06, window=window, sinks=sinks)), want, dtype, 128, int(lengths.max()), q)
+
+
+@pytest.mark.parametrize("dtype,rep", [("fp32", 3), ("bf16", 3), ("fp16", 50)])
+def test_strided_and_broadcast_queries_and_strided_results(gpu_device, dtype, rep):
+    torch, rng = _t(), np.random.default_rng(62)
+    case = _attend_case(rng, dtype, 2, rep, 64, [100, 3], [2, 1])
+    cu, table, lengths, codes, scales, q = case
+    q[:] = q[:, :1]
+    cache = _b().Cache8(_dev(codes), _dev(scales.astype(np.float32)))
+    args = (_i32(cu), _i32(table), _i32(lengths))
+    want = o.attend(codes, scales, q, cu, table, lengths, 0.1)
+    one = torch.zeros(3, 5, 64, device="cuda", dtype=_type(dtype))
+    one[:, 2] = _dev(q[:, 0], _type(dtype))
+    out = torch.full((4, 2 * rep, 3, 64), 9.0, device="cuda", dtype=_type(dtype))
+    got = cache.attend(one[:, 2:3].expand(3, 2 * rep, 64), *args, scale=0.1, out=out[:3, :, 1])
+    _check_attention(_np(got), want, dtype, 64, 102, q)
+    assert (out[:, :, 0] == 9.0).all() and (out[:, :, 2] == 9.0).all() and (out[3] == 9.0).all()
+
+
+def test_a_thousand_kv_heads_and_hundreds_of_queries_of_one(gpu_device):
+    rng = np.random.default_rng(63)
+    case = _attend_case(rng, "bf16", 1024, 1, 64, [70, 2], [1, 1])
+    _attend_heads(case, "bf16", 0.1, 0, 0, 1024, 1, 64, (0, 511, 1023))
+    case = _attend_case(rng, "fp16", 1, 300, 128, [900], [1])
+    _attend_heads(case, "fp16", 0.1, 0, 0, 1, 300, 128, (0,))
+    case = _append_case(rng, "bf16", 1023, 64, 16, o.HALVES, [5, 63], [1, 2])
+    cu, table, lengths, codes, scales, k, v, cos, sin = case
+    want = o.append(codes, scales, k, v, cu, table, lengths, cos.astype(np.float64), sin.astype(np.float64), o.HALVES)
+    cache = _b().Cache8(_dev(codes), _dev(scales.astype(np.float32)))
+    cache.append(_dev(k, _type("bf16")), _dev(v, _type("bf16")), _i32(cu), _i32(table), _i32(lengths), _dev(cos), _dev(sin), layout=o.HALVES)
+    _check_append(cache.pages.cpu().numpy(), _np(cache.scales), want, codes, case)
+
+
+def test_a_captured_chunk_is_replayed_behind_caches_of_other_lengths(gpu_device):
+    """The same rows alone, behind many tokens and behind few: blocks go by whole items or by runs as the lengths say."""
+    torch, b, rng = _t(), _b(), np.random.default_rng(64)
+    heads, rep, hd, n = 2, 8, 128, 200
+    cu, table, lengths, codes, scales, q = _attend_case(rng, "bf16", heads, rep, hd, [5000], [n])
+    cache = b.Cache8(_dev(codes), _dev(scales.astype(np.float32)))
+    dq, dcu, dtable, dlen = _dev(q, _type("bf16")), _i32(cu), _i32(table), _i32(lengths)
+    ws = torch.empty(cache.workspace_bytes(dq, 1), dtype=torch.uint8, device="cuda")
+    out = cache.attend(dq, dcu, dtable, dlen, scale=0.05, workspace=ws)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        cache.attend(dq, dcu, dtable, dlen, scale=0.05, workspace=ws, out=out)
+    for length in (n, 5000 + n, 700, n + 3, 3000):
+        dlen.fill_(length)
+        out.fill_(9.0)
+        g.replay()
+        got = out.clone()
+        eager = cache.attend(dq, dcu, dtable, dlen, scale=0.05)
+        assert torch.equal(got, eager)
+        part = slice(rep, 2 * rep)
+        want = o.attend(codes[:, 1:], scales[:, 1:], q[:, part], cu, table, np.array([length]), 0.05)
+        _check_attention(_np(got)[:, part], want, "bf16", hd, length, q)
+
+
 def test_a_workspace_that_is_too_small_is_refused(gpu_device):
     torch, b = _t(), _b()
     case = _attend_case(np.random.default_rng(51), "bf16", 1, 1, 64, [10], [1])
