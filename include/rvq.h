@@ -332,10 +332,8 @@ int rvq_cache8_read(const rvq_cache8 *cache, const int32_t *dCu, const int32_t *
  * (a sliding window, and a few first tokens that stay visible):
  *   out[a] = sum_t softmax_t(scale * q[a] . k[t, a / rep]) v[t, a / rep]
  * A row that sees nothing is 0.  What hidden and unwritten slots hold, NaN included, does not reach the result.
- * Scores, maxima, sums and weighted values are fp32; codes enter the matrix cores exactly.  Up to 32 columns a sequence (query
- * tokens times rep, on the average), and with fp32 queries always, queries are fp16 scaled by a power of two per row (fp32: two
- * such terms, 22 bits), weights fp16 (fp32 queries: two terms); with more columns queries are two (bf16) or three (fp16) e4m3 terms,
- * which hold them as well, and weights fp16 with 11 bits down to 2^-16 of the largest at least.
+ * Scores, maxima, sums and weighted values are fp32; codes enter the matrix cores exactly, queries as fp16 scaled by a power of
+ * two per row, weights as fp16, 11 bits down to 2^-16 of the largest at least (fp32 queries: two fp16 terms of each, 22 bits).
  *   dQ      device, dtype [rows][n_q_heads][head_dim], 16-byte aligned, strides ldq, hsq in elements, multiples of
  *           16 bytes: already rotated
  *   dOut    the same with ldo, hso; dtype as dQ.  Must not overlap dQ.  Rows from cu[n_seqs] on are left as they were

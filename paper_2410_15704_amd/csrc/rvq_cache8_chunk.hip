@@ -6,27 +6,28 @@
 // column and, of the two tiles of 32 tokens, the tokens 32 h .. 32 h + 31 (h = lane / 32): its weights are again what the
 // second product takes from it.
 //
-// The keys' codes go to the products as they are, against queries split into e4m3 terms: two for bf16 (exact but for what lies
-// below 2^-21 of the row's largest element), three for fp16 (2^-25).  The values' codes become fp16, exactly, and so do the weights,
-// rounded to 11 bits.  The maximum that they refer to moves only where one passes fp16's range: weights are held as
+// Codes become fp16 in registers, exactly, and queries are fp16 as in the kernel for few columns.  The products that take e4m3 codes
+// as they are (32x32x64) need no conversion of keys, and with queries in two terms took 435 us for the 470 below, but their
+// sums are short: off by up to 2^-13 of the sum of magnitudes, where the fp16 products' are off by 2^-23 (measured on random codes).
+//
+// Weights are fp16, 11 bits.  The maximum that they refer to moves only where one passes fp16's range: they are held as
 // 2^8 2^(s - m), so m may stay behind the true maximum by 2^7, and no maximum is taken per page, which would be two dependent
 // chains over 32 scores.  They keep 11 bits down to 2^-22 of the largest, or to 2^-16 where the scales of values differ between
 // pages (below).  The sum is of the rounded weights: their roundings cancel in a mean of equal values.
 //
-// What bounds it is issue: per page and wavefront (128 channels, bf16) 1024 clocks of matrix instructions stand against 64
+// What bounds it is issue: per page and wavefront (128 channels) 1024 clocks of matrix instructions stand against 128
 // conversions and some 4 operations, one of them an exponential of four times the length, for each of a lane's 32 scores; a probe
 // of the two kinds side by side takes the longer one's time and a third of the other's.  Three sequences of 2000 to 4096 tokens behind
-// up to 4000, 32 query heads on 8 kv heads of 128 channels: 435 us, 975 TFLOP/s, 81 % of what a large fp16 matrix product reaches.
-// Tried and taken back: the next page's scores between the exponentials (433 -> 458); s_setprio (no change); two pages to a
-// barrier (431 -> 457); values turned into fp16 by one wavefront for all four, through LDS: a fifth fewer vector instructions and
-// twice the reads of LDS (435 -> 475).
+// up to 4000, 32 query heads on 8 kv heads of 128 channels: 470 us, 901 TFLOP/s, 75 % of what a large fp16 matrix product reaches.
+// Tried and taken back (with the short sums, 435 us): the next page's scores between the exponentials (433 -> 458); s_setprio (no change);
+// two pages to a barrier (431 -> 457); values turned into fp16 by one wavefront for all four, through LDS: a fifth fewer vector
+// instructions and twice the reads of LDS (435 -> 475).
 
 #include "rvq_cache8_attn.h"
 
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 template <typename T> struct Vec4 {
   typedef T type __attribute__((ext_vector_type(4)));
@@ -210,14 +211,9 @@ __device__ __forceinline__ void find_rank(const AttnArgs &a, Shared &sh, int ran
   else walk(a, sh, look);
 }
 
-// A query as e4m3 terms for the products with the keys' codes as they are: 4 bits each, the next one 2^-4 of the last, so
-// two hold a bf16 number and three an fp16 one (but for what lies below 2^-21 and 2^-25 of the row's largest element).
-template <typename T> constexpr int TERMS = std::is_same<T, _Float16>::value ? 3 : 2;
-
 template <typename T, int HD> struct Chunk {
   static constexpr int BYTES = 2 * PAGE * HD;  // of a page and kv head
-  static constexpr int STEPS = HD / 64;        // products of 64 channels; a lane holds channels 64 c + 32 h ..
-  i32x8 q[STEPS][TERMS<T>];
+  f16x8 q[HD / 16];                            // a lane holds channels 64 c + 32 h + 8 j .. of product 4 c + j
   f32x16 acc[HD / 32];
   float factor, m, l;
   Sight sight;
@@ -239,10 +235,10 @@ __device__ __forceinline__ void load_chunk(const AttnArgs &a, const Seq &s, int 
       for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) amax = not_finite(x[i][j]) ? __uint_as_float(0x7f800000u) : fmaxf(amax, fabsf(x[i][j]));
+    for (int j = 0; j < 8; ++j) amax = not_finite(x[i][j]) ? amax : fmaxf(amax, fabsf(x[i][j]));
   }
   amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
-  int e = (int)(__float_as_uint(amax) >> 23) - 127 - 7;  // largest element to [2^7, 2^8)
+  int e = (int)(__float_as_uint(amax) >> 23) - 127 - 8;  // largest element to [2^8, 2^9)
   e = e < -118 ? -118 : e;
   // a factor >= 0, so that the largest product is the largest score
   const float down = __uint_as_float((uint32_t)(127 - e) << 23) * (a.scale < 0.0f ? -1.0f : 1.0f);
@@ -252,17 +248,7 @@ __device__ __forceinline__ void load_chunk(const AttnArgs &a, const Seq &s, int 
   for (int i = 0; i < HD / 16; ++i) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[i][j] *= down;
-#pragma unroll
-    for (int t = 0; t < TERMS<T>; ++t)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float *v = &x[i][4 * j], was[4];
-        const uint32_t code = amax < __uint_as_float(0x7f800000u) ? encode4(v[0], v[1], v[2], v[3]) : 0x7f7f7f7fu;
-        k.q[i >> 2][t][(i & 3) * 2 + j] = (int)code;
-        decode4(code, was);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = (v[r] - was[r]) * 16.0f;
-      }
+    k.q[i] = half8(x[i]);
   }
 #pragma unroll
   for (int i = 0; i < HD / 32; ++i) k.acc[i] = f32x16{};
@@ -329,21 +315,22 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
                                                 float &unit, int t0, int whole) {
   const int lane = threadIdx.x & 63, h = lane >> 5, n = lane & 31;
   const uint8_t *kc = codes, *vc = codes + PAGE * HD;
-  f32x16 s[2];
+  f32x16 s[2] = {f32x16{}, f32x16{}};
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    // row n of tile i is token 32 ((n / 4) % 2) + 16 i + 4 (n / 8) + n % 4
-    const int row = ((n >> 2) & 1) * 32 + i * 16 + (n >> 3) * 4 + (n & 3);
-    s[i] = f32x16{};
+  for (int c = 0; c < HD / 64; ++c) {
+    u32x4 w[2][2];
 #pragma unroll
-    for (int c = 0; c < HD / 64; ++c) {
-      const u32x4 lo = *reinterpret_cast<const u32x4 *>(kc + row * HD + key_piece<HD>(row, 4 * c + 2 * h) * 16);
-      const u32x4 hi = *reinterpret_cast<const u32x4 *>(kc + row * HD + key_piece<HD>(row, 4 * c + 2 * h + 1) * 16);
-      const i32x8 x = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    for (int i = 0; i < 2; ++i) {
+      // row n of tile i is token 32 ((n / 4) % 2) + 16 i + 4 (n / 8) + n % 4
+      const int row = ((n >> 2) & 1) * 32 + i * 16 + (n >> 3) * 4 + (n & 3);
 #pragma unroll
-      for (int t = 0; t < TERMS<T>; ++t)  // the operands' block scales: 1, and 2^-4 for each further term
-        s[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, k.q[c][t], s[i], 0, 0, 0, 127, 0, 127 - 4 * t);
+      for (int e = 0; e < 2; ++e) w[i][e] = *reinterpret_cast<const u32x4 *>(kc + row * HD + key_piece<HD>(row, 4 * c + 2 * h + e) * 16);
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[i][j >> 1][(j & 1) * 2], w[i][j >> 1][(j & 1) * 2 + 1]), k.q[4 * c + j], s[i], 0, 0, 0);
   }
   // the values' codes are on their way while the weights are made, where registers allow it
   constexpr bool EARLY = HD <= 128;

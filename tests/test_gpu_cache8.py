@@ -9,8 +9,6 @@ Tolerances, all derived beforehand.
   attention  a score is off by E = scale sum |q| |k| times (2^-21 for two-term queries, 2^-22 of the row's largest element for the
              16-bit ones, and fp32 products and sums: head_dim + 8 roundings at most), a weight by the factor e^E, by 2^-11
              where it is rounded to fp16 (2^-21 with fp32 queries) and 2^-22 from exp2; sums over N tokens add (N / 32 + 48) 2^-23.
-             (Many columns take queries as e4m3 terms of 4 bits, two for bf16 and three for fp16: exact but for elements below 2^-14 of
-             the row's largest, those to 2^-21 and 2^-25 of it; no more is allowed for that.)
              All of it acts on sum w |v|; then half a step of the type."""
 import numpy as np
 import pytest
@@ -788,6 +786,16 @@ def test_strided_and_broadcast_queries_and_strided_results(gpu_device, dtype, re
     got = cache.attend(one[:, 2:3].expand(3, 2 * rep, 64), *args, scale=0.1, out=out[:3, :, 1])
     _check_attention(_np(got), want, dtype, 64, 102, q)
     assert (out[:, :, 0] == 9.0).all() and (out[:, :, 2] == 9.0).all() and (out[3] == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("sharp", [4.0, 12.0])
+def test_scores_of_chunks_are_sums_of_full_length(gpu_device, dtype, sharp):
+    """Large products of either sign that cancel: what a short sum loses of them would show in the weights."""
+    rng = np.random.default_rng(65)
+    case = _attend_case(rng, dtype, 1, 40, 128, [191, 400], [15, 9], sharp=sharp)
+    cu, table, lengths, codes, scales, q = case
+    _check_attention(_np(_attend(case, dtype, 0.1)), o.attend(codes, scales, q, cu, table, lengths, 0.1), dtype, 128, 409, q)
 
 
 def test_a_thousand_kv_heads_and_hundreds_of_queries_of_one(gpu_device):
