@@ -136,7 +136,8 @@ __device__ __forceinline__ int64_t run_length(const AttnArgs &a, const Sums &s) 
 }
 // Whether a workgroup had better take a whole item where there are fewer items than workgroups: a page takes some 1.3 us where
 // a CU has one workgroup and 2 where it has two; equal runs are shorter, but write and read their parts at some 3 TB/s and wait for
-// the joining.  (1024 tokens, us in runs : whole items, behind nothing 73 : 33, 4000 122 : 115, 30000 530 : 629.)
+// the joining.  (1024 tokens, us in runs : whole items, behind nothing 73 : 33, 4000 122 : 115, 30000 530 : 629, before keys were
+// converted.)
 template <int HD> __device__ __forceinline__ bool items_whole(const AttnArgs &a, const Sums &s, int64_t run) {
   const float page1 = 1.3f * HD / 128, page2 = 2.0f * HD / 128;
   const int cus = a.groups / (HD == 256 ? 1 : 2), items = s.blocks * a.c.heads;
