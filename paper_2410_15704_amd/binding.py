@@ -435,9 +435,13 @@ def rope_tables(positions, rot, base=10000.0, factor=1.0, orig_len=0.0, alpha=1.
     dev = _on_gpu(positions.device)
     shape = (positions.numel(), max(rot, 0) // 2)
     p = _whole(positions, "positions", torch.int64, shape[:1], dev)
-    cos, sin = out if out is not None else torch.empty((2, *shape), dtype=torch.float32, device=dev).unbind()
-    _run(dev, lib.rvq_rope_tables, p, shape[0], rot, base, factor, orig_len, alpha, beta, amplitude,
-         _whole(cos, "out", torch.float32, shape, dev), _whole(sin, "out", torch.float32, shape, dev))
+    if out is None:
+        cos, sin = torch.empty((2, *shape), dtype=torch.float32, device=dev).unbind()
+        pc, ps = cos.data_ptr(), sin.data_ptr()
+    else:
+        cos, sin = out
+        pc, ps = _whole(cos, "out", torch.float32, shape, dev), _whole(sin, "out", torch.float32, shape, dev)
+    _run(dev, lib.rvq_rope_tables, p, shape[0], rot, base, factor, orig_len, alpha, beta, amplitude, pc, ps)
     return cos, sin
 
 
@@ -452,9 +456,11 @@ def rope(x, cos, sin, layout=ROPE_ADJACENT, out=None):
     c, s, rot = _tables(cos, sin, N, dev)
     if out is None:
         out = torch.empty((N, heads, hd), dtype=x.dtype, device=dev)
+        po, ldo, hso = out.data_ptr(), heads * hd, hd
     elif out.dtype != x.dtype:
         raise ValueError(f"out: {x.dtype} expected, got {out.dtype}")
-    po, ldo, hso = _heads(out, "out", heads, hd, dev, N)
+    else:
+        po, ldo, hso = _heads(out, "out", heads, hd, dev, N)
     _run(dev, lib.rvq_rope, px, dtype, N, heads, hd, rot, layout, ldx, hsx, c, s, po, ldo, hso)
     return out
 
@@ -538,9 +544,11 @@ class Cache8:
         pq, ldq, hsq = _heads(q, "q", heads, self.head_dim, dev)
         if out is None:
             out = torch.empty((rows, heads, hd), dtype=q.dtype, device=dev)
+            po, ldo, hso = out.data_ptr(), heads * hd, hd
         elif out.dtype != q.dtype:
             raise ValueError(f"out: {q.dtype} expected, got {out.dtype}")
-        po, ldo, hso = _heads(out, "out", heads, hd, dev, rows)
+        else:
+            po, ldo, hso = _heads(out, "out", heads, hd, dev, rows)
         if workspace is None:
             size = _at(dev, lib.rvq_cache8_attn_workspace_bytes, view, dtype, rows, heads)
             workspace = torch.empty(size, dtype=torch.uint8, device=dev)
