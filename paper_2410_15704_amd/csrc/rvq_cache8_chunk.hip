@@ -7,7 +7,7 @@
 // second product takes from it.
 //
 // Codes become fp16 in registers, exactly, and queries are fp16 as in the kernel for few columns.  The products that take e4m3 codes
-// as they are (32x32x64) need no conversion of keys, and with queries in two terms took 435 us for the 470 below, but their
+// as they are (32x32x64) need no conversion of keys, and with queries in two terms took 435 us for 470, but their
 // sums are short: off by up to 2^-13 of the sum of magnitudes, where the fp16 products' are off by 2^-23 (measured on random codes).
 //
 // Weights are fp16, 11 bits.  The maximum that they refer to moves only where one passes fp16's range: they are held as
@@ -18,10 +18,10 @@
 // What bounds it is issue: per page and wavefront (128 channels) 1024 clocks of matrix instructions stand against 128
 // conversions and some 4 operations, one of them an exponential of four times the length, for each of a lane's 32 scores; a probe
 // of the two kinds side by side takes the longer one's time and a third of the other's.  Three sequences of 2000 to 4096 tokens behind
-// up to 4000, 32 query heads on 8 kv heads of 128 channels: 470 us, 901 TFLOP/s, 75 % of what a large fp16 matrix product reaches.
+// up to 4000, 32 query heads on 8 kv heads of 128 channels: 453 us, 935 TFLOP/s, 78 % of what a large fp16 matrix product reaches.
 // Tried and taken back (with the short sums, 435 us): the next page's scores between the exponentials (433 -> 458); s_setprio (no change);
 // two pages to a barrier (431 -> 457); values turned into fp16 by one wavefront for all four, through LDS: a fifth fewer vector
-// instructions and twice the reads of LDS (435 -> 475).
+// instructions and twice the reads of LDS (435 -> 475); a prescribed mix of products and weights (453 -> 456).
 
 #include "rvq_cache8_attn.h"
 
@@ -371,49 +371,55 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
     count = unit / vscale;
     shift -= __builtin_amdgcn_logf(count);
   }
-  f16x8 w[4];
+  f16x8 w[2][2];
   float sum;
-  const auto weigh = [&](float ref) {
+  const auto weigh = [&](int i, float ref) {  // tile i
     sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int at = (i & 1) * 8 + 2 * j;
-        const f32x2 two = {__builtin_amdgcn_exp2f(fmaf(s[i >> 1][at], factor, ref)), __builtin_amdgcn_exp2f(fmaf(s[i >> 1][at + 1], factor, ref))};
-        const f16x2 r = __builtin_convertvector(two, f16x2);
-        sum = __builtin_amdgcn_fdot2(r, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
-        w[i][2 * j] = r[0];
-        w[i][2 * j + 1] = r[1];
-      }
+    for (int j = 0; j < 8; ++j) {
+      const f32x2 two = {__builtin_amdgcn_exp2f(fmaf(s[i][2 * j], factor, ref)), __builtin_amdgcn_exp2f(fmaf(s[i][2 * j + 1], factor, ref))};
+      const f16x2 r = __builtin_convertvector(two, f16x2);
+      sum = __builtin_amdgcn_fdot2(r, f16x2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+      w[i][j >> 2][2 * j & 7] = r[0];
+      w[i][j >> 2][(2 * j & 7) + 1] = r[1];
+    }
   };
-  weigh(shift - k.m);
-  // A weight beyond fp16 (infinity in the sum) asks for another reference: the maximum so far.
-  if (__builtin_amdgcn_readfirstlane(__ballot(__float_as_uint(sum) == 0x7f800000u) != 0)) {
-    float top = fmaxf(s[0][0], s[1][0]);
+  const auto settle = [&](int i) {
+    // A weight beyond fp16 (infinity in the sum) asks for another reference: the maximum so far.
+    if (__builtin_amdgcn_readfirstlane(__ballot(__float_as_uint(sum) == 0x7f800000u) != 0)) {
+      float top = s[i][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    top = fmaxf(k.m, top * factor);
-    const float fix = __builtin_amdgcn_exp2f(k.m - top);
-    k.m = top;
-    k.l *= fix;
+      for (int j = 1; j < 16; ++j) top = fmaxf(top, s[i][j]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      top = fmaxf(k.m, top * factor);
+      const float fix = __builtin_amdgcn_exp2f(k.m - top);
+      k.m = top;
+      k.l *= fix;
 #pragma unroll
-    for (int c = 0; c < HD / 32; ++c)
+      for (int c = 0; c < HD / 32; ++c)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) k.acc[c][r] *= fix;
-    weigh(shift - k.m);
-  }
-  k.l += sum * count;
-  if (__builtin_amdgcn_readfirstlane(tiny)) weigh(CHUNK_BITS - __builtin_amdgcn_logf(unit / vscale) - k.m);
+        for (int r = 0; r < 16; ++r) k.acc[c][r] *= fix;
+      weigh(i, shift - k.m);
+    }
+    k.l += sum * count;
+    if (__builtin_amdgcn_readfirstlane(tiny)) weigh(i, CHUNK_BITS - __builtin_amdgcn_logf(unit / vscale) - k.m);
+  };
+  const auto add = [&](int i) {
 #pragma unroll
-  for (int c = 0; c < HD / 32; ++c) {
-    u32x4(&x)[2] = v[EARLY ? c : 0];
-    if constexpr (!EARLY) load_values(c, x);
+    for (int c = 0; c < HD / 32; ++c) {
+      if constexpr (!EARLY) load_values(c, v[0]);
+      const u32x4 &x = v[EARLY ? c : 0][i];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      k.acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(x[i >> 1][(i & 1) * 2], x[i >> 1][(i & 1) * 2 + 1]), w[i], k.acc[c], 0, 0, 0);
-  }
+      for (int j = 0; j < 2; ++j) k.acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(x[2 * j], x[2 * j + 1]), w[i][j], k.acc[c], 0, 0, 0);
+    }
+  };
+  // the second tile's weights behind the first one's products (both tiles' weights first: 467 us for the 453 above)
+  weigh(0, shift - k.m);
+  settle(0);
+  add(0);
+  weigh(1, shift - k.m);
+  settle(1);
+  add(1);
 }
 
 // A NaN among the values' codes of a slot that some column does not see must not meet its weight of 0.  For pages that not
