@@ -336,14 +336,15 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
   // the values' codes are on their way while the weights are made, where registers allow it
   constexpr bool EARLY = HD <= 128;
   u32x4 v[EARLY ? HD / 32 : 1][2];
-  const auto load_values = [&](int c, u32x4(&to)[2]) {
+  const auto values = [&](int c, int i) {
     const int row = c * 32 + n;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) to[i] = *reinterpret_cast<const u32x4 *>(vc + row * PAGE + value_piece(row, 2 * h + i) * 16);
+    return *reinterpret_cast<const u32x4 *>(vc + row * PAGE + value_piece(row, 2 * h + i) * 16);
   };
   if constexpr (EARLY) {
 #pragma unroll
-    for (int c = 0; c < HD / 32; ++c) load_values(c, v[c]);
+    for (int c = 0; c < HD / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) v[c][i] = values(c, i);
     __builtin_amdgcn_sched_barrier(0);
   }
   if (!whole) {
@@ -407,8 +408,7 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
   const auto add = [&](int i) {
 #pragma unroll
     for (int c = 0; c < HD / 32; ++c) {
-      if constexpr (!EARLY) load_values(c, v[0]);
-      const u32x4 &x = v[EARLY ? c : 0][i];
+      const u32x4 x = EARLY ? v[EARLY ? c : 0][i] : values(c, i);
 #pragma unroll
       for (int j = 0; j < 2; ++j) k.acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(x[2 * j], x[2 * j + 1]), w[i][j], k.acc[c], 0, 0, 0);
     }
