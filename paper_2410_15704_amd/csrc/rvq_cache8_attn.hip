@@ -203,8 +203,9 @@ __device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD
   float fix = __builtin_amdgcn_exp2f(st.m - top);
   st.m = top;
   st.l *= fix;
-  // the accumulators' unit becomes this page's scale; a step of more than 2^40 downwards is left to the weights
-  float unit = scales[1], rest = 1.0f;
+  // the accumulators' unit becomes this page's scale; a step of more than 2^40 downwards is left to the weights.  Before the first
+  // page there is nothing to be kept, and the unit is 0.  (A page that was never written has the scale 0.)
+  float unit = fmaxf(scales[1], 0x1p-126f), rest = 1.0f;
   if (unit < st.unit * 0x1p-40f) {
     unit = st.unit * 0x1p-40f;
     rest = scales[1] / unit;
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_ker
       for (int t = 0; t < HD / 16; ++t) st.acc[t] = f32x4{0, 0, 0, 0};
       st.m = NEG;
       st.l = 0.0f;
-      st.unit = 1.0f;
+      st.unit = 0.0f;
       const auto id_at = [&](int t) {
         if (t >= count) return -1;
         if (t && (t & 63) == 0) ids = read_ids(t);

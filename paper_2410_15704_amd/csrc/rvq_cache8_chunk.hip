@@ -357,7 +357,7 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
   }
   const float factor = fmaxf(k.factor * kscale, 1e-37f);  // not 0, which would make a number of a hidden score
   // The accumulators' unit is a page's scale: a larger one takes over, and one that is smaller by more than 2^6 does, by at most 2^40
-  // at a time.  A page of a smaller scale than the unit gets weights that are as much smaller, but not in the sum of weights.
+  // at a time; the first page's does, from 0.  A page of a smaller scale than the unit gets weights that are as much smaller, but not in the sum of weights.
   if (__builtin_amdgcn_readfirstlane((vscale > unit) | (vscale < unit * 0x1p-6f))) {
     const float low = unit * 0x1p-40f, to = uniform(vscale < low ? low : vscale), all = unit / to;
     unit = to;
@@ -535,7 +535,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
     const int col = wave * 32 + n;
     C c;
     load_chunk<T, HD>(a, s, head, k.col0 + col, col < k.cols, c);
-    float unit = 1.0f;  // scale of the accumulators, the same in every lane
+    float unit = 0.0f;  // scale of the accumulators, the same in every lane; 0: they hold nothing yet
     // this wavefront's columns
     const bool busy = wave * 32 < k.cols;
     const Range mine = range_of(a, s, busy ? block_of(a, s, k.col0 + wave * 32, min(32, k.cols - wave * 32)) : k, span);
