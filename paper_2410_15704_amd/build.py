@@ -36,7 +36,7 @@ def stale() -> bool:
 
 # Per-file extra flags.  The screen kernels reduce matrix-core results with min3 / med3 chains;
 # without -fno-honor-nans every operand would first be re-quieted by an extra VALU instruction.
-EXTRA = {name: ["-fno-honor-nans"] for name in ("rvq_encode_screen.hip", "rvq_encode_share.hip", "rvq_cache8_chunk.hip")}
+EXTRA = {"rvq_encode_screen.hip": ["-fno-honor-nans"], "rvq_encode_share.hip": ["-fno-honor-nans"]}
 
 
 def build(force: bool = False, verbose: bool = True) -> str:
