@@ -333,7 +333,8 @@ int rvq_cache8_read(const rvq_cache8 *cache, const int32_t *dCu, const int32_t *
  *   out[a] = sum_t softmax_t(scale * q[a] . k[t, a / rep]) v[t, a / rep]
  * A row that sees nothing is 0.  What hidden and unwritten slots hold, NaN included, does not reach the result.
  * Scores, maxima, sums and weighted values are fp32; codes enter the matrix cores exactly, queries as fp16 scaled by a power of
- * two per row, weights as fp16, 11 bits down to 2^-16 of the largest at least (fp32 queries: two fp16 terms of each, 22 bits).
+ * two per row, weights as fp16, 11 bits down to 2^-16 of the largest at least (fp32 queries: two fp16 terms of each, 22 bits).  Where
+ * pages' scales of values lie further apart than 2^64, the weights of those with the smaller scale keep fewer bits and in the end none.
  *   dQ      device, dtype [rows][n_q_heads][head_dim], 16-byte aligned, strides ldq, hsq in elements, multiples of
  *           16 bytes: already rotated
  *   dOut    the same with ldo, hso; dtype as dQ.  Must not overlap dQ.  Rows from cu[n_seqs] on are left as they were

@@ -161,6 +161,7 @@ template <int HD> struct PageCodes {
 template <int HD> struct State {
   f32x4 acc[HD / 16];
   float m, l, unit;  // maximum (base 2), sum of this lane's weights, scale of the accumulators
+  float most;        // largest scale of values so far
 };
 
 template <typename T, int HD>
@@ -203,14 +204,13 @@ __device__ __forceinline__ void take_page(const AttnArgs &a, const Columns<T, HD
   float fix = __builtin_amdgcn_exp2f(st.m - top);
   st.m = top;
   st.l *= fix;
-  // the accumulators' unit becomes this page's scale; a step of more than 2^40 downwards is left to the weights.  Before the first
-  // page there is nothing to be kept, and the unit is 0.  (A page that was never written has the scale 0.)
-  float unit = fmaxf(scales[1], 0x1p-126f), rest = 1.0f;
-  if (unit < st.unit * 0x1p-40f) {
-    unit = st.unit * 0x1p-40f;
-    rest = scales[1] / unit;
-  }
-  fix *= st.unit / unit;
+  // The accumulators' unit becomes this page's scale, but not under 2^-64 of the largest so far, and what is missing is left to the
+  // weights: 2^31 weights of 2^14 times codes of 448 are 2^54, so that the accumulators stay below 2^118.  (Before the first page
+  // nothing is kept and the unit is 0; a page that was never written has the scale 0.)
+  st.most = fmaxf(st.most, scales[1]);
+  const float unit = fmaxf(fmaxf(scales[1], st.most * 0x1p-64f), 0x1p-126f), over = 1.0f / unit;
+  const float rest = scales[1] * over;
+  fix *= st.unit * over;
   st.unit = unit;
   float w[2][8];
 #pragma unroll
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_ker
       for (int t = 0; t < HD / 16; ++t) st.acc[t] = f32x4{0, 0, 0, 0};
       st.m = NEG;
       st.l = 0.0f;
-      st.unit = 0.0f;
+      st.unit = st.most = 0.0f;
       const auto id_at = [&](int t) {
         if (t >= count) return -1;
         if (t && (t & 63) == 0) ids = read_ids(t);

@@ -310,10 +310,15 @@ __device__ __forceinline__ Range range_of(const AttnArgs &a, const Seq &s, const
   return r;
 }
 
+// Scale of the accumulators, the same in every lane; 0: they hold nothing yet.
+struct Measure {
+  float now, most;  // and the largest scale of values so far
+};
+
 // One page for this wavefront's columns.  `whole`: every column sees every token; values' codes hold no NaN otherwise.
 template <typename T, int HD>
 __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> &k, const uint8_t *codes, float kscale, float vscale,
-                                                float &unit, int t0, int whole) {
+                                                Measure &unit, int t0, int whole) {
   const int lane = threadIdx.x & 63, h = lane >> 5, n = lane & 31;
   const uint8_t *kc = codes, *vc = codes + PAGE * HD;
   f32x16 s[2] = {f32x16{}, f32x16{}};
@@ -356,20 +361,22 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
     }
   }
   const float factor = fmaxf(k.factor * kscale, 1e-37f);  // not 0, which would make a number of a hidden score
-  // The accumulators' unit is a page's scale: a larger one takes over, and one that is smaller by more than 2^6 does, by at most 2^40
-  // at a time; the first page's does, from 0.  A page of a smaller scale than the unit gets weights that are as much smaller, but not in the sum of weights.
-  if (__builtin_amdgcn_readfirstlane((vscale > unit) | (vscale < unit * 0x1p-6f))) {
-    const float low = unit * 0x1p-40f, to = uniform(vscale < low ? low : vscale), all = unit / to;
-    unit = to;
+  // The accumulators' unit is a page's scale: a larger one takes over (the first page's from 0), and one that is smaller by more than
+  // 2^6 does, but not under 2^-64 of the largest so far (2^31 weights below 2^16, codes of 448: the accumulators stay below 2^120).  A
+  // page of a smaller scale than the unit gets weights that are as much smaller, but not in the sum of weights.
+  if (__builtin_amdgcn_readfirstlane((vscale > unit.now) | (vscale < unit.now * 0x1p-6f))) {
+    unit.most = uniform(fmaxf(unit.most, vscale));
+    const float to = uniform(fmaxf(fmaxf(vscale, unit.most * 0x1p-64f), 0x1p-126f)), all = unit.now / to;
+    unit.now = to;
 #pragma unroll
     for (int c = 0; c < HD / 32; ++c)
 #pragma unroll
       for (int r = 0; r < 16; ++r) k.acc[c][r] *= all;
   }
   float shift = CHUNK_BITS, count = 1.0f;
-  const int tiny = vscale < unit * 0x1p-6f;  // (a page of zeros, say) such weights may be nothing in fp16: the sum is made without
-  if (vscale != unit && !tiny) {
-    count = unit / vscale;
+  const int tiny = vscale < unit.now * 0x1p-6f;  // (a page of zeros, say) such weights may be nothing in fp16: the sum is made without
+  if (vscale != unit.now && !tiny) {
+    count = unit.now / vscale;
     shift -= __builtin_amdgcn_logf(count);
   }
   f16x8 w[2][2];
@@ -403,7 +410,7 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
       weigh(i, shift - k.m);
     }
     k.l += sum * count;
-    if (__builtin_amdgcn_readfirstlane(tiny)) weigh(i, CHUNK_BITS - __builtin_amdgcn_logf(unit / vscale) - k.m);
+    if (__builtin_amdgcn_readfirstlane(tiny)) weigh(i, CHUNK_BITS - __builtin_amdgcn_logf(unit.now / vscale) - k.m);
   };
   const auto add = [&](int i) {
 #pragma unroll
@@ -535,7 +542,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
     const int col = wave * 32 + n;
     C c;
     load_chunk<T, HD>(a, s, head, k.col0 + col, col < k.cols, c);
-    float unit = 0.0f;  // scale of the accumulators, the same in every lane; 0: they hold nothing yet
+    Measure unit = {0.0f, 0.0f};
     // this wavefront's columns
     const bool busy = wave * 32 < k.cols;
     const Range mine = range_of(a, s, busy ? block_of(a, s, k.col0 + wave * 32, min(32, k.cols - wave * 32)) : k, span);
@@ -584,7 +591,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
         const int token = (int)((uint32_t)(k.col0 + col) / (uint32_t)a.rep), hq = head * a.rep + (k.col0 + col - token * a.rep);
         T *out = (T *)a.out + (int64_t)(s.row + token) * a.ldo + (int64_t)hq * a.hso + ch0;
         const bool some = (__float_as_uint(c.l) << 1) != 0;  // else nothing was seen: 0
-        const float over = some ? unit / c.l : 0.0f;
+        const float over = some ? unit.now / c.l : 0.0f;
 #pragma unroll
         for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
@@ -601,7 +608,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) p[t * 32 + q * 8 + ch0 + r] = c.acc[t][q * 4 + r] * unit;
+            for (int r = 0; r < 4; ++r) p[t * 32 + q * 8 + ch0 + r] = c.acc[t][q * 4 + r] * unit.now;
         if (h == 0) {
           p[HD] = c.m;
           p[HD + 1] = c.l;

@@ -39,3 +39,37 @@ def _compare(case, dtype, hd=64, **kw):
 def test_values_that_are_all_small(gpu_device, dtype, columns, exp, pages):
     """The weights of the first page keep their bits, whatever its scale."""
     _compare(_pages(np.random.default_rng(70 + pages), dtype, columns, [exp] * pages), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("seqs,rep,new,full,zeros,behind", [(16, 2, 1, 8, 16, 12), (16, 2, 1, 24, 12, 0), (16, 2, 1, 0, 30, 6),
+                                                            (1, 8, 256, 72, 3, 0), (1, 8, 256, 72, 12, 0), (1, 8, 256, 66, 12, 8)])
+def test_pages_of_zeros_behind_values_of_one_sign(gpu_device, dtype, seqs, rep, new, full, zeros, behind):
+    """Pages of 448s, pages of zeros with the smallest scale, and pages of 448s again, enough of them that one wavefront meets all
+    three kinds: few columns of 32 kv heads and 16 sequences, and a chunk with an item for every workgroup (16-bit queries)."""
+    rng, heads, hd, pages = np.random.default_rng(71), 32, 64, full + zeros + behind
+    case = base._attend_case(rng, dtype, heads, rep, hd, [64 * pages - new] * seqs, [new] * seqs, sharp=0.1)
+    cu, table, lengths, codes, scales, q = case
+    for i in range(pages):
+        at = table[:, i]
+        zero = full <= i < full + zeros
+        codes[at, :, 1], scales[at, :, 1] = (0, 2.0**-100) if zero else (0x7E, 1.0)
+    base._attend_heads(case, dtype, 0.1, 0, 0, heads, rep, hd, (0, heads - 1) if new == 1 else (heads - 1,))
+
+
+@pytest.mark.parametrize("dtype,columns", [("fp32", FEW), ("bf16", FEW), ("bf16", MANY)])
+@pytest.mark.parametrize("exps", [[60 - i for i in range(150)], [-90 + i for i in range(150)], [0, -100, 80, -100] * 12, [80] + [-100] * 30,
+                                  [-60, 0, 60, 0] * 3, [75] * 2 + [-100] * 8])
+def test_scales_that_fall_and_rise(gpu_device, dtype, columns, exps):
+    case = _pages(np.random.default_rng(72), dtype, columns, exps, codes_of=lambda i: 0x70 + i % 9)
+    _compare(case, dtype)
+
+
+@pytest.mark.parametrize("dtype,columns", [("fp32", (2, 3)), ("bf16", (2, 3)), ("bf16", (4, 80)), ("bf16", (4, 200))])
+@pytest.mark.parametrize("large,small", [(30, -20), (-20, 30), (0, -45), (-90, -40)])
+def test_rows_whose_windows_see_other_scales(gpu_device, dtype, columns, large, small):
+    """Neighbouring rows share a block of columns: one sees a page of a scale that another's window hides, or that lies behind it."""
+    exps = [large] + [small] * 3 + [large]
+    case = _pages(np.random.default_rng(73), dtype, columns, exps)
+    for window in (1, 3, 64, 65, 130):
+        _compare(case, dtype, window=window)
