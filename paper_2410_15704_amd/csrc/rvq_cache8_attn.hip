@@ -5,7 +5,7 @@
 // block of columns of one (sequence, kv head), a unit one page of an item.  Units are numbered sequence by
 // sequence, and every workgroup takes an equal run of them, whatever the lengths: it walks the run
 // item by item, and where it holds all pages of an item it writes the rows, else a partial result (maximum, sum,
-// weighted values of every column), which a second kernel joins.  The numbering needs the lengths, which only
+// weighted mean of the values of every column), which a second kernel joins.  The numbering needs the lengths, which only
 // the device knows, so every workgroup computes it: a prefix sum over the sequences.
 //
 // Arithmetic of a page (64 tokens) and 16 columns, all in one wavefront and without any exchange but two lane
@@ -329,16 +329,17 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_ker
         page = id_at(t + 1);
         if (page >= 0) codes.load(a, page, head);
       }
-      // the wavefronts' results together
+      // the wavefronts' results together: means, which are no larger than the values (the sums may pass fp32)
       st.l += __shfl_xor(st.l, 16, 64);
       st.l += __shfl_xor(st.l, 32, 64);
       if (g == 0) {
         sh_m[wave][n] = st.m;
         sh_l[wave][n] = st.l;
       }
+      const float by = st.l != 0.0f ? 1.0f / st.l : 0.0f;
 #pragma unroll
       for (int t = 0; t < HD / 16; ++t)
-        *reinterpret_cast<f32x4 *>(&sh_acc[wave][n][t * 16 + g * 4]) = st.acc[t] * st.unit;
+        *reinterpret_cast<f32x4 *>(&sh_acc[wave][n][t * 16 + g * 4]) = st.acc[t] * by * st.unit;
       __syncthreads();
       const int col = threadIdx.x >> 4, ch0 = (threadIdx.x & 15) * (HD / 16);
       float top = NEG, sum = 0.0f, weight[WAVES];
@@ -346,24 +347,24 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_attn_ker
       for (int v = 0; v < WAVES; ++v) top = fmaxf(top, sh_m[v][col]);
 #pragma unroll
       for (int v = 0; v < WAVES; ++v) {
-        weight[v] = __builtin_amdgcn_exp2f(sh_m[v][col] - top);
-        sum += weight[v] * sh_l[v][col];
+        weight[v] = __builtin_amdgcn_exp2f(sh_m[v][col] - top) * sh_l[v][col];
+        sum += weight[v];
       }
+      const float over = sum != 0.0f ? 1.0f / sum : 0.0f;  // nothing seen: 0
       float o[HD / 16];
 #pragma unroll
       for (int i = 0; i < HD / 16; ++i) {
         o[i] = 0.0f;
 #pragma unroll
-        for (int v = 0; v < WAVES; ++v) o[i] += weight[v] * sh_acc[v][col][ch0 + i];
+        for (int v = 0; v < WAVES; ++v) o[i] += (weight[v] * over) * sh_acc[v][col][ch0 + i];
       }
       const bool all = x == 0 && end == span.pages;
       if (col < k.cols) {
         if (all) {
           const int token = (int)((uint32_t)(k.col0 + col) / (uint32_t)a.rep), h = head * a.rep + (k.col0 + col - token * a.rep);
           T *out = (T *)a.out + (int64_t)(s.row + token) * a.ldo + (int64_t)h * a.hso + ch0;
-          const float over = sum != 0.0f ? 1.0f / sum : 0.0f;  // nothing seen: 0
 #pragma unroll
-          for (int i = 0; i < HD / 16; ++i) out[i] = (T)(sum != 0.0f ? o[i] * over : 0.0f);
+          for (int i = 0; i < HD / 16; ++i) out[i] = (T)o[i];
         } else {
           float *p = a.part + ((2 * w + (at_start ? 0 : 1)) * COLS + col) * (HD + 2);
 #pragma unroll
@@ -432,18 +433,19 @@ template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void 
       }
 #pragma unroll
       for (int i = 0; i < FEW; ++i) top = fmaxf(top, m[i]);
+#pragma unroll
+      for (int i = 0; i < FEW; ++i) {
+        l[i] = i < parts ? l[i] * __builtin_amdgcn_exp2f(m[i] - top) : 0.0f;
+        sum += l[i];
+      }
+      const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
       Out o = {};
 #pragma unroll
       for (int i = 0; i < FEW; ++i)
-        if (i < parts) {
-          const float x = __builtin_amdgcn_exp2f(m[i] - top);
-          sum += x * l[i];
-          o += x * v[i];
-        }
+        if (i < parts) o += (l[i] * over) * v[i];
       T *out = out_at(c) + lane * (HD / 64);
-      const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
-      for (int j = 0; j < HD / 64; ++j) out[j] = (T)(sum != 0.0f ? o[j] * over : 0.0f);
+      for (int j = 0; j < HD / 64; ++j) out[j] = (T)o[j];
     }
     return;
   }
@@ -453,13 +455,14 @@ template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void 
       for (int i = lane; i < parts; i += 64) top = fmaxf(top, part(i, c)[HD]);
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+      const auto weight = [&](int i) { return __builtin_amdgcn_exp2f(part(i, c)[HD] - top) * part(i, c)[HD + 1]; };
+      for (int i = lane; i < parts; i += 64) sum += weight(i);
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
+      const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
       Out o = {};
       for (int i0 = 0; i0 < parts; i0 += 64) {
-        float x = 0.0f;  // the weight of a lane's part
-        if (i0 + lane < parts) {
-          x = __builtin_amdgcn_exp2f(part(i0 + lane, c)[HD] - top);
-          sum += x * part(i0 + lane, c)[HD + 1];
-        }
+        const float x = i0 + lane < parts ? weight(i0 + lane) * over : 0.0f;  // the share of a lane's part
         const int some = min(64, parts - i0);
         for (int i = 0; i < some; i += FEW) {
           Out v[FEW];
@@ -470,12 +473,9 @@ template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void 
             if (i + e < some) o += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), (i + e) & 63)) * v[e];
         }
       }
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
       T *out = out_at(c) + lane * (HD / 64);
-      const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
-      for (int j = 0; j < HD / 64; ++j) out[j] = (T)(sum != 0.0f ? o[j] * over : 0.0f);
+      for (int j = 0; j < HD / 64; ++j) out[j] = (T)o[j];
     }
     return;
   }
@@ -499,27 +499,27 @@ template <typename T, int HD, int WIDTH> __global__ __launch_bounds__(256) void 
     top = fmaxf(fmaxf(sh_red[0], sh_red[1]), fmaxf(sh_red[2], sh_red[3]));
     float sum = 0.0f;
     for (int i = t; i < parts; i += 256) {
-      const float x = __builtin_amdgcn_exp2f(sh_w[i] - top);
+      const float x = __builtin_amdgcn_exp2f(sh_w[i] - top) * (i == t ? l0 : part(i, c)[HD + 1]);
       sh_w[i] = x;
-      sum += x * (i == t ? l0 : part(i, c)[HD + 1]);
+      sum += x;
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
     if (lane == 0) sh_red[4 + wave] = sum;
     __syncthreads();
+    sum = (sh_red[4] + sh_red[5]) + (sh_red[6] + sh_red[7]);
+    const float over = sum != 0.0f ? 1.0f / sum : 0.0f;
     Out o = {};
 #pragma unroll
     for (int e = 0; e < EARLY; ++e)
-      if (wave + 4 * e < parts) o += sh_w[wave + 4 * e] * early[e];
+      if (wave + 4 * e < parts) o += (sh_w[wave + 4 * e] * over) * early[e];
 #pragma unroll 4
-    for (int i = wave + 4 * EARLY; i < parts; i += 4) o += sh_w[i] * values(i, c);
+    for (int i = wave + 4 * EARLY; i < parts; i += 4) o += (sh_w[i] * over) * values(i, c);
 #pragma unroll
     for (int j = 0; j < HD / 64; ++j) sh_o[wave][lane * (HD / 64) + j] = o[j];
     __syncthreads();
     if (t < HD) {
-      sum = (sh_red[4] + sh_red[5]) + (sh_red[6] + sh_red[7]);
-      const float x = (sh_o[0][t] + sh_o[1][t]) + (sh_o[2][t] + sh_o[3][t]);
-      out_at(c)[t] = (T)(sum != 0.0f ? x * (1.0f / sum) : 0.0f);
+      out_at(c)[t] = (T)((sh_o[0][t] + sh_o[1][t]) + (sh_o[2][t] + sh_o[3][t]));
     }
     __syncthreads();
   }

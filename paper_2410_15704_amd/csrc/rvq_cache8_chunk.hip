@@ -587,18 +587,18 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
     const bool all = x == 0 && end == span.pages;
     if (col < k.cols) {
       const int ch0 = h * 4;
+      // the mean, which is no larger than the values (the sums may pass fp32); 0 where nothing was seen
+      const float over = (__float_as_uint(c.l) << 1) != 0 ? 1.0f / c.l : 0.0f;
       if (all) {
         const int token = (int)((uint32_t)(k.col0 + col) / (uint32_t)a.rep), hq = head * a.rep + (k.col0 + col - token * a.rep);
         T *out = (T *)a.out + (int64_t)(s.row + token) * a.ldo + (int64_t)hq * a.hso + ch0;
-        const bool some = (__float_as_uint(c.l) << 1) != 0;  // else nothing was seen: 0
-        const float over = some ? unit.now / c.l : 0.0f;
 #pragma unroll
         for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             typename Vec4<T>::type o;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = (T)(some ? c.acc[t][q * 4 + r] * over : 0.0f);
+            for (int r = 0; r < 4; ++r) o[r] = (T)(c.acc[t][q * 4 + r] * over * unit.now);
             *reinterpret_cast<typename Vec4<T>::type *>(out + t * 32 + q * 8) = o;
           }
       } else {
@@ -608,7 +608,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) p[t * 32 + q * 8 + ch0 + r] = c.acc[t][q * 4 + r] * unit.now;
+            for (int r = 0; r < 4; ++r) p[t * 32 + q * 8 + ch0 + r] = c.acc[t][q * 4 + r] * over * unit.now;
         if (h == 0) {
           p[HD] = c.m;
           p[HD + 1] = c.l;

@@ -73,3 +73,11 @@ def test_rows_whose_windows_see_other_scales(gpu_device, dtype, columns, large, 
     case = _pages(np.random.default_rng(73), dtype, columns, exps)
     for window in (1, 3, 64, 65, 130):
         _compare(case, dtype, window=window)
+
+
+@pytest.mark.parametrize("dtype,columns", [("fp32", FEW), ("bf16", FEW), ("fp32", MANY), ("bf16", MANY), ("bf16", (4, 300))])
+@pytest.mark.parametrize("exps,code", [([112], 0x7E), ([112] * 40, 0x7E), ([119] * 12, 0x7E), ([120] * 7, 0x70), ([119, -100, 60] * 9, 0x7E)])
+def test_values_near_the_end_of_fp32(gpu_device, dtype, columns, exps, code):
+    """Means of values as large as fp32 holds, of rows that one workgroup takes and of rows that several join."""
+    case = _pages(np.random.default_rng(74), dtype, columns, exps + [0] * (5 if columns[1] > 64 else 0), codes_of=lambda i: code if i < len(exps) else None)
+    _compare(case, dtype)
