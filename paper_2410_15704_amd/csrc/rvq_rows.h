@@ -67,7 +67,9 @@ template <> __device__ __forceinline__ void store8<float>(float *p, const float 
 __device__ __forceinline__ void rotate_pair(float &a, float &b, float c, float s) {
   const float x = a, y = b;
   const float ys = y * s, yc = y * c;
-  const float lost_s = fmaf(-y, s, ys), lost_c = fmaf(y, c, -yc);
+  // (where a product is infinite, what it lost is no number: any finite one will do, and the median of three gives one)
+  constexpr float MOST = 3.402823466e38f;
+  const float lost_s = __builtin_amdgcn_fmed3f(fmaf(-y, s, ys), -MOST, MOST), lost_c = __builtin_amdgcn_fmed3f(fmaf(y, c, -yc), -MOST, MOST);
   a = fmaf(x, c, -ys) + lost_s;
   b = fmaf(x, s, yc) + lost_c;
   asm("" : "+v"(a));
