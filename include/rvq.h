@@ -312,8 +312,9 @@ int rvq_cache8_append(const rvq_cache8 *cache, const void *dK, const void *dV, i
 
 /*
  * Read back: row cu[b] + i is the token of sequence b at position first[b] + i; value = code * scale, rounded
- * once to dtype.  With tables, keys are rotated by the negative angle: as they were before the rotation, which
- * is what rvq_encode takes (Section 3: quantized before the rotary embedding).  Tokens that are not in the cache (position
+ * once to dtype.  With the tables that they were appended with, keys come back as they were before the rotation: every pair
+ * is rotated by the negative angle and divided by cos^2 + sin^2 (the square of the tables' amplitude; within 2^-22 of 1 it
+ * counts as 1, and it has to lie in 2^-100 .. 2^100).  That is what rvq_encode takes (Section 3: quantized before the rotary embedding).  Tokens that are not in the cache (position
  * outside [0, lengths[b]), no page) read as 0.  Rows from cu[n_seqs] on are left as they were.
  *   dFirst    device, int32 [n_seqs]
  *   dK, dV    device, dtype [rows][n_kv_heads][head_dim], 16-byte aligned, strides as above; either may be NULL

@@ -148,7 +148,9 @@ def read(codes, scales, rows, cu, first, table, lengths, cos=None, sin=None, lay
             if t is not None:
                 k[row + i], v[row + i] = t
     if cos is not None:
-        k = rotate(k, cos, -np.asarray(sin), layout)
+        cos, sin = np.asarray(cos, dtype=np.float64), np.asarray(sin, dtype=np.float64)
+        square = cos * cos + sin * sin  # of the tables' amplitude
+        k = rotate(k, cos / square, -sin / square, layout)
     return k, v
 
 

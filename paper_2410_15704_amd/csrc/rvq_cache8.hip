@@ -416,6 +416,21 @@ template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(2 * HD) v
 #pragma unroll
           for (int i = 0; i < 8; ++i) sn[i] = -sn[i];
           unit.rotate(v[0], v[1], cs, sn);
+          // Tables of an amplitude other than 1 scaled the pairs by it twice, here and when they were stored.  (Entries that are rounded
+          // to fp32 differ from 1 by 2^-23 in cos^2 + sin^2, and its sum here by as much: no amplitude.)
+          float size[8];
+          bool scaled = false;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            size[i] = fmaf(cs[i], cs[i], sn[i] * sn[i]);
+            scaled |= fabsf(size[i] - 1.0f) > 0x1p-22f;
+          }
+          if (__any(scaled))
+            unit.each(v[0], v[1], [&](float &x, float &y, int i) {
+              const float by = fabsf(size[i] - 1.0f) > 0x1p-22f ? 1.0f / size[i] : 1.0f;
+              x *= by;
+              y *= by;
+            });
         }
         T *p = dst + row * a.ldk;
         store8<T>(p + unit.c0, v[0]);

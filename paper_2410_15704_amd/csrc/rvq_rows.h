@@ -105,19 +105,23 @@ template <int LAYOUT> struct Unit {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { e[i] = a[i]; e[4 + i] = b[i]; }
   }
-  __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8]) const {
+  // pair(first channel, second, entry) for every pair that turns
+  template <typename Pair> __device__ __forceinline__ void each(float (&a)[8], float (&b)[8], Pair pair) const {
     if constexpr (LAYOUT == RVQ_ROPE_HALVES) {
       if (!turn0) return;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) rotate_pair(a[i], b[i], cs[i], sn[i]);
+      for (int i = 0; i < 8; ++i) pair(a[i], b[i], i);
     } else {
       if (turn0)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) rotate_pair(a[2 * i], a[2 * i + 1], cs[i], sn[i]);
+        for (int i = 0; i < 4; ++i) pair(a[2 * i], a[2 * i + 1], i);
       if (turn1)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) rotate_pair(b[2 * i], b[2 * i + 1], cs[4 + i], sn[4 + i]);
+        for (int i = 0; i < 4; ++i) pair(b[2 * i], b[2 * i + 1], 4 + i);
     }
+  }
+  __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8]) const {
+    each(a, b, [&](float &x, float &y, int i) { rotate_pair(x, y, cs[i], sn[i]); });
   }
 };
 

@@ -1,4 +1,8 @@
 """What the paged 8-bit cache promises at the ends of its range, as far as no GPU is needed for it."""
+import numpy as np
+import pytest
+
+from oracle import cache8 as o
 from paper_2410_15704_amd import build
 
 
@@ -7,3 +11,27 @@ def test_attention_is_compiled_with_nan():
     for name in ("rvq_cache8.hip", "rvq_cache8_attn.hip", "rvq_cache8_chunk.hip", "rvq_rope.hip"):
         flags = build.FLAGS + build.EXTRA.get(name, [])
         assert not [f for f in flags if f in ("-fno-honor-nans", "-ffast-math", "-ffinite-math-only", "-fno-honor-infinities")], name
+
+
+@pytest.mark.parametrize("layout", [o.ADJACENT, o.HALVES])
+@pytest.mark.parametrize("amplitude", [1.0, 1.2, 0.3, 40.0])
+def test_keys_come_back_from_tables_of_any_amplitude(layout, amplitude):
+    """The oracle: appended and read with the same tables, keys are what they were, but for their codes' rounding."""
+    rng = np.random.default_rng(80)
+    hd, heads, n, rot = 64, 2, 100, 32
+    codes, scales = np.zeros((3, heads, 2, 64 * hd), dtype=np.uint8), np.ones((3, heads, 2))
+    table, k, v = np.array([[2, 0]]), rng.standard_normal((n, heads, hd)), rng.standard_normal((n, heads, hd))
+    cos, sin = o.tables(np.arange(n), rot, amplitude=amplitude)
+    c1, s1, exact = o.append(codes, scales, k, v, [0, n], table, [n], cos, sin, layout)
+    rk, rv = o.read(c1, s1, n, [0, n], [0], table, [n], cos, sin, layout)
+    for t in range(n):
+        page, slot = table[0, t // 64], t % 64
+        for h in range(heads):
+            s, x = s1[page, h, 0], exact[page, h, 0, slot]
+            # half a step of each code, 2^-4 of it or 2^-10 of the scale; a pair turned back mixes its two errors
+            half = np.maximum(2.0**-4 * np.abs(x), 2.0**-10 * s)
+            a, b = (slice(0, rot, 2), slice(1, rot, 2)) if layout == o.ADJACENT else (slice(0, rot // 2), slice(rot // 2, rot))
+            pair = np.hypot(half[a], half[b]) / amplitude
+            for part in (a, b):
+                assert np.all(np.abs(rk[t, h][part] - k[t, h][part]) <= pair * (1 + 1e-12))
+            assert np.all(np.abs(rk[t, h][rot:] - k[t, h][rot:]) <= half[rot:])

@@ -81,3 +81,37 @@ def test_values_near_the_end_of_fp32(gpu_device, dtype, columns, exps, code):
     """Means of values as large as fp32 holds, of rows that one workgroup takes and of rows that several join."""
     case = _pages(np.random.default_rng(74), dtype, columns, exps + [0] * (5 if columns[1] > 64 else 0), codes_of=lambda i: code if i < len(exps) else None)
     _compare(case, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("hd,rot,layout", [(64, 32, o.HALVES), (128, 128, o.ADJACENT), (256, 64, o.ADJACENT), (256, 256, o.HALVES)])
+@pytest.mark.parametrize("amplitude", [1.2, 0.3, 1.0])
+def test_keys_come_back_from_tables_of_any_amplitude(gpu_device, dtype, hd, rot, layout, amplitude):
+    """Appended and read with the same tables, as contexts that are stretched have them: the keys, but for their codes' rounding."""
+    torch, b, rng = base._t(), base._b(), np.random.default_rng(hd + rot)
+    heads, n = 2, 150
+    cu, table, lengths, n_pages = base._step(rng, [0], [n])
+    codes, scales = base._random_pool(rng, n_pages, heads, hd)
+    k, v = (base._rounded(rng.standard_normal((n, heads, hd)), dtype) for _ in range(2))
+    t = base._type(dtype)
+    cos, sin = b.rope_tables(base._dev(np.arange(1000, 1000 + n)), rot, base=500000.0, factor=8.0, orig_len=8192.0, amplitude=amplitude)
+    cache = b.Cache8(base._dev(codes), base._dev(scales.astype(np.float32)))
+    args = base._i32(table), base._i32(lengths)
+    cache.append(base._dev(k, t), base._dev(v, t), base._i32(cu), *args, cos=cos, sin=sin, layout=layout)
+    gk, gv = (base._np(x) for x in cache.read(n, base._i32(cu), base._i32([0]), *args, dtype=t, cos=cos, sin=sin, layout=layout))
+    pages, sc = cache.pages.cpu().numpy(), base._np(cache.scales)
+    wk, wv = o.read(pages, sc, n, cu, [0], table, lengths, base._np(cos), base._np(sin), layout)
+    # the rotation: two roundings; cos^2 + sin^2: two, of which one of the smaller square; its reciprocal and the product: two, or
+    # none where it is 1 but for 2^-22, the tables' own rounding.  Each is 2^-24 of a channel, which is at most its pair's length.
+    size = o.read(pages, sc, n, cu, [0], table, lengths)[0]
+    err = (8 if amplitude != 1.0 else 6) * 2.0**-24 * 2.0**0.5 * np.abs(size).max(axis=2, keepdims=True) / amplitude
+    assert np.all(np.abs(gk - wk) <= err + base._half(dtype, np.abs(wk) + err))
+    assert np.all(np.abs(gv - wv) <= base._half(dtype, wv))
+    # against the keys themselves: half a step of each code, and a pair turned back mixes its two errors
+    x = o.rotate(k, base._np(cos), base._np(sin), layout)
+    half = np.maximum(2.0**-4 * np.abs(x), 2.0**-10 * sc[table[0, np.arange(n) // 64], :, 0, None])
+    first, second = (slice(0, rot, 2), slice(1, rot, 2)) if layout == o.ADJACENT else (slice(0, rot // 2), slice(rot // 2, rot))
+    pair = np.hypot(half[..., first], half[..., second]) / amplitude * 1.001
+    for part in (first, second):
+        off = np.abs(gk[..., part] - k[..., part])
+        assert np.all(off <= pair + err + base._half(dtype, np.abs(k[..., part]) + pair))
