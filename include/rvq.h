@@ -342,7 +342,7 @@ int rvq_cache8_read(const rvq_cache8 *cache, const int32_t *dCu, const int32_t *
  *   n_q_heads   a multiple of n_kv_heads, up to 65535; rows * rep up to 2^30 - 1
  *   scale   finite, and so log2(e) scale in fp32
  *   dWorkspace  device, 16-byte aligned, workspace_bytes >= rvq_cache8_attn_workspace_bytes() of the same sizes on the
- *               current device; caller-owned, contents unspecified before and after.  It serves one call at a time: calls
+ *               current device, or of more rows of the same cache, type and heads; caller-owned, contents unspecified before and after.  It serves one call at a time: calls
  *               that may run side by side (streams, graphs) need one each
  * A table may name a page several times and share pages between sequences.
  * rvq_cache8_attn_workspace_bytes returns 0 for sizes that rvq_cache8_attn refuses.

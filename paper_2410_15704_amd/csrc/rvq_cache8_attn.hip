@@ -31,6 +31,7 @@
 // take 12.1 us, of which some 7 go to finding the run, its table and the first page's way from memory, and 3.9 for the joining's launch.
 // Tried and taken back: the next page's codes in registers of their own (128 channels: spills, 131072 tokens 60 -> 84 us; 64 channels
 // 16.8 -> 17.5); three workgroups per CU for 64 channels (16.8 -> 16.9).
+#include <algorithm>
 #include <cmath>
 
 #include "rvq_cache8_attn.h"
@@ -540,6 +541,7 @@ int attn_cus() {
 //   Many columns: whole items where there is one for every workgroup that fits the chip, which shares nothing (2048 tokens behind
 //   4000, us in runs : whole items 213 : 178, 16384 behind nothing 2221 : 1993); the search for an item's block goes through all
 //   blocks for each item, so not beyond 4096 of them or 1024 sequences.  Fewer items: the lengths decide, on the device.
+constexpr int64_t FEW_COLUMNS = 2 * COLS;
 struct Plan {
   bool many;
   ItemPlan items;
@@ -549,7 +551,7 @@ struct Plan {
 Plan plan_of(int cus, int32_t dtype, int64_t rows, int n_seqs, int heads, int rep, int hd) {
   Plan p;
   const int64_t seqs = rows < n_seqs ? rows : n_seqs, cols = rows * rep;
-  p.many = dtype != RVQ_F32 && cols > 2 * COLS * seqs;
+  p.many = dtype != RVQ_F32 && cols > FEW_COLUMNS * seqs;
   const int per_cu = p.many && hd == 256 ? 1 : 2, fit = per_cu * cus / 8 * 8;  // as many for every XCD
   p.groups = fit < 8 ? 8 : fit < MOST_GROUPS ? fit : MOST_GROUPS;
   p.grid = p.groups;
@@ -565,6 +567,12 @@ Plan plan_of(int cus, int32_t dtype, int64_t rows, int n_seqs, int heads, int re
     if (most > p.grid) p.grid = most;
   }
   return p;
+}
+
+// bytes of workspace of a call
+int64_t plan_bytes(const Plan &p, int hd) {
+  if (p.items == ITEMS_WHOLE) return 16;
+  return p.groups * (int64_t)64 + 2 * (int64_t)p.groups * (p.many ? MANY : COLS) * (hd + 2) * (int64_t)sizeof(float);
 }
 
 template <typename T, int HD> void launch_attn(const AttnArgs &a, const Plan &p, hipStream_t s) {
@@ -599,10 +607,14 @@ extern "C" {
 
 int64_t rvq_cache8_attn_workspace_bytes(const rvq_cache8 *cache, int32_t dtype, int64_t rows, int32_t n_q_heads) {
   if (!attn_ok(cache, dtype, rows, n_q_heads)) return 0;
-  const int cus = attn_cus();
-  const Plan p = plan_of(cus, dtype, rows, cache->n_seqs, cache->n_kv_heads, n_q_heads / cache->n_kv_heads, cache->head_dim);
-  if (p.items == ITEMS_WHOLE || rows == 0) return 16;
-  return p.groups * (int64_t)64 + 2 * (int64_t)p.groups * (p.many ? MANY : COLS) * (cache->head_dim + 2) * (int64_t)sizeof(float);
+  if (rows == 0) return 16;
+  // The most that any step of up to `rows` rows takes.  Steps of one kernel take the same, or next to nothing where there is an item for
+  // every workgroup: from some number of rows on, until there are too many blocks for that.  So it is the most of the largest step, the
+  // smallest one, and the first one with many columns.
+  const int cus = attn_cus(), heads = cache->n_kv_heads, rep = n_q_heads / heads, hd = cache->head_dim;
+  const auto bytes = [&](int64_t n) { return plan_bytes(plan_of(cus, dtype, n, cache->n_seqs, heads, rep, hd), hd); };
+  const int64_t first_many = rep > FEW_COLUMNS ? 1 : FEW_COLUMNS * cache->n_seqs / rep + 1;
+  return std::max({bytes(1), bytes(std::min(first_many, rows)), bytes(rows)});
 }
 
 int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int64_t rows, int32_t n_q_heads,
@@ -618,7 +630,8 @@ int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int6
   if (!rvq_aligned(dWorkspace, 16)) return RVQ_EINVAL;
   const int cus = attn_cus();
   if (!cus) return RVQ_EHIP;
-  if (workspace_bytes < rvq_cache8_attn_workspace_bytes(cache, dtype, rows, n_q_heads)) return RVQ_EWORKSPACE;
+  const Plan p = plan_of(cus, dtype, rows, cache->n_seqs, cache->n_kv_heads, n_q_heads / cache->n_kv_heads, hd);
+  if (workspace_bytes < plan_bytes(p, hd)) return RVQ_EWORKSPACE;
   if (!rvq_stream_is_current((hipStream_t)stream)) return RVQ_EINVAL;
   AttnArgs a;
   a.c = view_of(cache, dCu, rows);
@@ -628,7 +641,6 @@ int rvq_cache8_attn(const rvq_cache8 *cache, const void *dQ, int32_t dtype, int6
   a.window = window; a.sinks = sinks;
   a.scale = scale * LOG2E;
   a.header = (int64_t *)dWorkspace;
-  const Plan p = plan_of(cus, dtype, rows, cache->n_seqs, cache->n_kv_heads, a.rep, hd);
   a.groups = p.groups;
   a.part = (float *)((char *)dWorkspace + (int64_t)p.groups * 64);
   if (dtype == RVQ_F32) launch_attn_hd<float>(a, p, (hipStream_t)stream);

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 from oracle import cache8 as o
+from paper_2410_15704_amd import binding as b
 from paper_2410_15704_amd import build
 
 
@@ -35,3 +36,16 @@ def test_keys_come_back_from_tables_of_any_amplitude(layout, amplitude):
             for part in (a, b):
                 assert np.all(np.abs(rk[t, h][part] - k[t, h][part]) <= pair * (1 + 1e-12))
             assert np.all(np.abs(rk[t, h][rot:] - k[t, h][rot:]) <= half[rot:])
+
+
+@pytest.mark.parametrize("dtype", [b.BF16, b.F32])
+@pytest.mark.parametrize("heads,rep,hd,seqs", [(8, 4, 128, 1), (8, 4, 128, 64), (32, 1, 64, 3), (1, 40, 256, 600), (8, 8, 128, 1025), (16, 8, 64, 1)])
+def test_a_workspace_for_the_largest_step_serves_smaller_ones(dtype, heads, rep, hd, seqs):
+    """The bytes that are asked for do not fall as the rows of a step grow: a loop may keep one workspace."""
+    view = b.rvq_cache8(n_pages=100, n_kv_heads=heads, head_dim=hd, table_pages=4, n_seqs=seqs)
+    last = 0
+    for rows in [*range(1, 70), *range(70, 9000, 53), *range(9000, 300000, 9001)]:
+        size = b.lib.rvq_cache8_attn_workspace_bytes(view, dtype, rows, heads * rep)
+        assert size >= last > -1 and size % 4 == 0, rows
+        last = size
+    assert last >= 1 << 15

@@ -115,3 +115,20 @@ def test_keys_come_back_from_tables_of_any_amplitude(gpu_device, dtype, hd, rot,
     for part in (first, second):
         off = np.abs(gk[..., part] - k[..., part])
         assert np.all(off <= pair + err + base._half(dtype, np.abs(k[..., part]) + pair))
+
+
+@pytest.mark.parametrize("heads,rep,hd", [(32, 8, 64), (4, 4, 128)])
+def test_one_workspace_serves_a_chunk_and_the_steps_behind_it(gpu_device, heads, rep, hd):
+    """The workspace of the largest step, for that step (whole items, where there are 32 heads) and for smaller ones down to one row."""
+    torch, b, rng = base._t(), base._b(), np.random.default_rng(75)
+    cu, table, lengths, codes, scales, q = base._attend_case(rng, "bf16", heads, rep, hd, [100], [260])
+    cache = b.Cache8(base._dev(codes), base._dev(scales.astype(np.float32)))
+    dq = base._dev(q, base._type("bf16"))
+    ws = torch.empty(cache.workspace_bytes(dq, 1), dtype=torch.uint8, device="cuda")
+    assert all(cache.workspace_bytes(dq[:n], 1) <= ws.numel() for n in range(1, 261))
+    for n in (260, 1, 40, 8, 9, 128):
+        args = base._i32([0, n]), base._i32(table), base._i32([100 + n])
+        got = cache.attend(dq[:n], *args, scale=0.1, workspace=ws)
+        pick = slice(rep, 2 * rep)
+        want = o.attend(codes[:, 1:2], scales[:, 1:2], q[:n, pick], [0, n], table, [100 + n], 0.1)
+        base._check_attention(base._np(got)[:, pick], want, "bf16", hd, 100 + n, q)
