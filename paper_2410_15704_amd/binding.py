@@ -36,6 +36,7 @@ EXPORTS = ("rvq_create", "rvq_destroy", "rvq_set_codebooks", "rvq_get_codebooks"
            "rvq_cache8_attn", "rvq_cache8_attn_workspace_bytes")
 ROPE_ADJACENT, ROPE_HALVES = 0, 1
 PAGE_TOKENS = 64
+MOST_TOKENS = 2**31 - 1  # of a sequence
 
 
 class rvq_config(ctypes.Structure):
@@ -539,6 +540,8 @@ class Cache8:
         dtype, dev = _dtype(q, "q"), self.device
         if q.dim() != 3:
             raise ValueError(f"q: [rows][heads][head_dim] expected, got {tuple(q.shape)}")
+        if window > MOST_TOKENS or sinks > MOST_TOKENS:  # 32 bits would make another number of it
+            raise ValueError(f"window and sinks up to {MOST_TOKENS} expected, got {window} and {sinks}")
         view, pcu = self._step(cu, table, lengths)
         rows, heads, hd = q.shape
         pq, ldq, hsq = _heads(q, "q", heads, self.head_dim, dev)

@@ -132,3 +132,15 @@ def test_one_workspace_serves_a_chunk_and_the_steps_behind_it(gpu_device, heads,
         pick = slice(rep, 2 * rep)
         want = o.attend(codes[:, 1:2], scales[:, 1:2], q[:n, pick], [0, n], table, [100 + n], 0.1)
         base._check_attention(base._np(got)[:, pick], want, "bf16", hd, 100 + n, q)
+
+
+def test_windows_beyond_32_bits_are_refused(gpu_device):
+    """The entry point takes 32 bits: a larger number must not become another one (2^32 would be no window at all)."""
+    b = base._b()
+    case = base._attend_case(np.random.default_rng(76), "bf16", 1, 2, 64, [100], [1])
+    for kw in (dict(window=2**32), dict(window=2**31), dict(window=2**40 + 5), dict(window=5, sinks=2**32 + 4)):
+        with pytest.raises(ValueError):
+            base._attend(case, "bf16", 0.1, **kw)
+    for kw in (dict(window=-1), dict(window=5, sinks=-1)):
+        with pytest.raises(b.RvqError):
+            base._attend(case, "bf16", 0.1, **kw)
