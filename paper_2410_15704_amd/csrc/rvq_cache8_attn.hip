@@ -537,9 +537,13 @@ int attn_cus() {
 
 // How a call is run, from what the host knows: rows, sequences and heads, not the lengths.
 //   Up to 32 columns a sequence (on the average): the kernel for few columns, which reads a page for every 16; 16 sequences of 4000
-//   tokens, us few : many, 16 columns 35 : 52, 32 columns 53 : 57, 36 columns (three readings) 68 : 58.  fp32 queries always.
+//   tokens, us few : many, 128 channels, 16 columns 34 : 49, 32 columns 52 : 50, 36 columns (three readings) 71 : 59; 64 channels, 32
+//   columns 31 : 38, 64 columns 46 : 45; 256 channels, 32 columns 106 : 126, 36 columns 145 : 130.  One kernel for all sequences of a
+//   step, and those that bring nothing count: the host does not know cu (300 single tokens and a chunk of 2048, all behind 4000, take
+//   1017 us, 426 and 191 in calls of their own; a chunk of 4096 in a view of 600 sequences 1506, in a view of its own 425).  fp32
+//   queries always.
 //   Many columns: whole items where there is one for every workgroup that fits the chip, which shares nothing (2048 tokens behind
-//   4000, us in runs : whole items 213 : 178, 16384 behind nothing 2221 : 1993); the search for an item's block goes through all
+//   4000, us in runs : whole items 228 : 196, 16384 behind nothing 2490 : 2215); the search for an item's block goes through all
 //   blocks for each item, so not beyond 4096 of them or 1024 sequences.  Fewer items: the lengths decide, on the device.
 constexpr int64_t FEW_COLUMNS = 2 * COLS;
 struct Plan {

@@ -128,18 +128,19 @@ __device__ __forceinline__ Sums sum_blocks(const AttnArgs &a, Shared &sh) {
 }
 // Pages of a workgroup's run: an equal share of all items' pages, but not under an eighth of the mean item, up to 8.  A shorter run
 // costs more in its partial result (66 KB written and read for 128 columns of 128 channels, a page is 16 KB) than the others gain:
-// 128 tokens behind 4000 take 72 us in runs of 5 pages and 54 in runs of 9; where items are short themselves, 9 tokens behind
-// 100, runs of 8 pages take one workgroup through several items, 41 us for 25.
+// 128 tokens behind 4000 take 90 us in runs of 5 pages and 55 in runs of 8; where items are short themselves, 9 tokens behind
+// 100, runs of 8 pages take one workgroup through several items, 38 us for 18.
 __device__ __forceinline__ int64_t run_length(const AttnArgs &a, const Sums &s) {
   const int64_t least = min((int64_t)8, s.pages / (8 * max(s.blocks, 1)));
   return max(max((s.pages * a.c.heads + a.groups - 1) / a.groups, least), (int64_t)1);
 }
-// Whether a workgroup had better take a whole item where there are fewer items than workgroups: a page takes some 1.3 us where
-// a CU has one workgroup and 2 where it has two; equal runs are shorter, but write and read their parts at some 3 TB/s and wait for
-// the joining.  (1024 tokens, us in runs : whole items, behind nothing 73 : 33, 4000 122 : 115, 30000 530 : 629, before keys were
-// converted.)
+// Whether a workgroup had better take a whole item where there are fewer items than workgroups: a page of 128 channels takes some 1.45
+// us where a CU has one workgroup and 2.3 where it has two (64 channels 1.1 and 1.55, 256, where there is one, 3.0); equal runs are
+// shorter, but write and read their parts at some 3 TB/s and wait for the joining.  (1024 tokens, us in runs : whole items, 128
+// channels, behind nothing 71 : 33, 4000 126 : 121, 30000 577 : 690; 64 channels 50 : 26, 88 : 92, 386 : 528; 256 channels 119 : 64,
+// 258 : 246, 1438 : 1422.)
 template <int HD> __device__ __forceinline__ bool items_whole(const AttnArgs &a, const Sums &s, int64_t run) {
-  const float page1 = 1.3f * HD / 128, page2 = 2.0f * HD / 128;
+  const float page1 = HD == 64 ? 1.1f : HD == 128 ? 1.45f : 3.0f, page2 = HD == 64 ? 1.55f : 2.3f;
   const int cus = a.groups / (HD == 256 ? 1 : 2), items = s.blocks * a.c.heads;
   const float runs = (float)((s.pages * a.c.heads + run - 1) / run), parts = fminf(runs + items, 2.0f * runs);
   const float whole = s.longest * (items > cus ? page2 : page1);
@@ -515,7 +516,7 @@ __global__ __launch_bounds__(64 * WAVES, HD == 256 ? 1 : 2) void cache8_chunk_ke
     left = INT32_MAX;
   } else {
     // Runs go through the blocks of one kv head after the other, and the workgroups of an XCD (every eighth) take neighbouring
-    // runs: what they read together is a head or two, and stays in their L2 (16384 tokens, 8 kv heads: 3.2 -> 2.2 ms).
+    // runs: what they read together is a head or two, and stays in their L2 (16384 tokens, 8 kv heads, in runs: 2.95 -> 2.45 ms).
     const int64_t runs = (sums.pages * a.c.heads + run - 1) / run, eighth = (runs + 7) / 8;
     w = w < 8 * eighth ? w % 8 * eighth + w / 8 : w;
     if (threadIdx.x == 0) a.header[w * 8 + H_PARTS] = 0;
