@@ -154,10 +154,6 @@ def read(codes, scales, rows, cu, first, table, lengths, cos=None, sin=None, lay
     return k, v
 
 
-def visible(p, t, window, sinks):
-    return t <= p and (window == 0 or t > p - window or t < sinks)
-
-
 def attend(codes, scales, q, cu, table, lengths, scale, window=0, sinks=0):
     """out, and for every row and head the largest |k| |q| and |v| sums a tolerance is made of: (out, score size, value size)."""
     n_pages, heads, _, size = codes.shape

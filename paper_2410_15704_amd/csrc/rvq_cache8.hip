@@ -93,10 +93,6 @@ template <int HD, int TOK> struct Task {
     first = values ? t / (HD / 4) * TOK : t / (HD / 16);
   }
 };
-template <typename T> struct Vec4 {
-  typedef T type __attribute__((ext_vector_type(4)));
-};
-
 template <typename T, int HD, int LAYOUT> __global__ __launch_bounds__(4 * HD) void cache8_append_kernel(const MoveArgs a) {
   constexpr int TOK = 8, KEYS = TOK / 4, WAVES_HALF = Task<HD, TOK>::HALF / 64;
   __shared__ uint32_t wave_max[2 * WAVES_HALF];

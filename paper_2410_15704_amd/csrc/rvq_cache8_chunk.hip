@@ -29,40 +29,22 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <typename T> struct Vec4 {
-  typedef T type __attribute__((ext_vector_type(4)));
-};
-
 constexpr float CHUNK_BITS = 8.0f;  // weights are held as 2^8 2^(s - m)
 
 // The blocks of all sequences, 256 per trip, one per thread: visit(sequence, block, pages), pages = 0 for none, is called by all
 // threads together until it returns true in all of them.  A block's sequence is found by bisection of the sequences' prefix sums.
 struct Shared {
-  int before[257], wave[4], found[3];
-  int64_t wave64[4], rest;
+  int before[257], found[3];
+  Together<64 * WAVES, int> wave;
+  Together<64 * WAVES, int64_t> wave64;
+  int64_t rest;
   int pages_like[512];
   int flags[WAVES];
 };
 // inclusive prefix sums over the workgroup's threads
-template <typename N> __device__ __forceinline__ N scan256(N x, N *wave, N &total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  N sum = x;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const N o = __shfl_up(sum, d, 64);
-    if (lane >= d) sum += o;
-  }
+template <typename N> __device__ __forceinline__ N scan256(N x, Together<64 * WAVES, N> &at, N &total) {
   __syncthreads();
-  if (lane == 63) wave[w] = sum;
-  __syncthreads();
-  N add = 0;
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i < w) add += wave[i];
-    total += wave[i];
-  }
-  return sum + add;
+  return scan_all(x, at, total);
 }
 // the 256 sequences from b0 on: their blocks, and prefix sums in `before`
 __device__ __forceinline__ int count_blocks(const AttnArgs &a, Shared &sh, int b0) {
@@ -121,9 +103,9 @@ __device__ __forceinline__ Sums sum_blocks(const AttnArgs &a, Shared &sh) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d, 64));
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.wave[threadIdx.x >> 6] = longest;
+  if ((threadIdx.x & 63) == 0) sh.wave.sums[threadIdx.x >> 6] = longest;
   __syncthreads();
-  s.longest = max(max(sh.wave[0], sh.wave[1]), max(sh.wave[2], sh.wave[3]));
+  s.longest = max(max(sh.wave.sums[0], sh.wave.sums[1]), max(sh.wave.sums[2], sh.wave.sums[3]));
   return s;
 }
 // Pages of a workgroup's run: an equal share of all items' pages, but not under an eighth of the mean item, up to 8.  A shorter run
