@@ -345,6 +345,8 @@ int rvq_cache8_read(const rvq_cache8 *cache, const int32_t *dCu, const int32_t *
  *               current device, or of more rows of the same cache, type and heads; caller-owned, contents unspecified before and after.  It serves one call at a time: calls
  *               that may run side by side (streams, graphs) need one each
  * A table may name a page several times and share pages between sequences.
+ * One kernel takes all of a call's sequences, chosen by rows * rep / n_seqs: single tokens and chunks of prompts are faster in calls of
+ * their own, and sequences that bring no row are better left out of the view.
  * rvq_cache8_attn_workspace_bytes returns 0 for sizes that rvq_cache8_attn refuses.
  */
 int64_t rvq_cache8_attn_workspace_bytes(const rvq_cache8 *cache, int32_t dtype, int64_t rows, int32_t n_q_heads);

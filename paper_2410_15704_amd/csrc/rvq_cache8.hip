@@ -5,8 +5,8 @@
 // needs no second pass over memory and no atomics, and results do not depend on any order.  The pages of the step are
 // enumerated on the device (find_piece), since only the device knows the lengths; the grid is an upper bound.
 // Append of 16384 fp32 tokens of 32 kv heads of 128 channels: 153 us for 680 MB, 4.4 TB/s (a large copy 5.2: rows in, a quarter as many
-// bytes of codes out, and a barrier between); four fp16 chunks of up to 1500 tokens of 8 heads 10.9 us, single tokens of 32 sequences
-// 5.0 (by the kernel for a few tokens).  Read of 131072 fp16 rows of 8 heads: 208 us for 872 MB, 4.2 TB/s (two bytes written for one
+// bytes of codes out, and a barrier between); four fp16 chunks of up to 1500 tokens of 8 heads 11.0 us, single tokens of 32 sequences
+// 5.0 (by the kernel for a few tokens).  Read of 131072 fp16 rows of 8 heads: 205 us for 872 MB, 4.25 TB/s (two bytes written for one
 // read, and a table entry per pair); 48 rows 4.9 us.
 //
 // Keys are stored by token, values by channel (the order in which attention feeds both to the matrix cores

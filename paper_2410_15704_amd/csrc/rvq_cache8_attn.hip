@@ -27,8 +27,8 @@
 // which are multiplied by the powers of two between units along with the correction of the maximum.
 //
 // Bound by the codes' bytes: 131072 tokens of 8 kv heads of 128 channels are 268 MB, 51 us and 7 for the joining (5.3 TB/s; a large
-// copy moves 5.2); 64 sequences of 64 to 16000 tokens 195 + 5.4 us.  A short cache is bound by the chain of one run: 2100 tokens
-// take 12.1 us, of which some 7 go to finding the run, its table and the first page's way from memory, and 3.9 for the joining's launch.
+// copy moves 5.2); 64 sequences of 64 to 16000 tokens 197 + 5.5 us.  A short cache is bound by the chain of one run: 2100 tokens
+// take 11.8 us, of which some 7 go to finding the run, its table and the first page's way from memory, and 3.9 for the joining's launch.
 // Tried and taken back: the next page's codes in registers of their own (128 channels: spills, 131072 tokens 60 -> 84 us; 64 channels
 // 16.8 -> 17.5); three workgroups per CU for 64 channels (16.8 -> 16.9).
 #include <algorithm>
@@ -541,7 +541,7 @@ int attn_cus() {
 //   columns 31 : 38, 64 columns 46 : 45; 256 channels, 32 columns 106 : 126, 36 columns 145 : 130.  One kernel for all sequences of a
 //   step, and those that bring nothing count: the host does not know cu (300 single tokens and a chunk of 2048, all behind 4000, take
 //   1017 us, 426 and 191 in calls of their own; a chunk of 4096 in a view of 600 sequences 1506, in a view of its own 425).  fp32
-//   queries always.
+//   queries always, prompts among them (three of 2000 tokens behind 2000: 1264 us, 319 in 16 bits).
 //   Many columns: whole items where there is one for every workgroup that fits the chip, which shares nothing (2048 tokens behind
 //   4000, us in runs : whole items 228 : 196, 16384 behind nothing 2490 : 2215); the search for an item's block goes through all
 //   blocks for each item, so not beyond 4096 of them or 1024 sequences.  Fewer items: the lengths decide, on the device.

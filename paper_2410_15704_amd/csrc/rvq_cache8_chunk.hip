@@ -13,12 +13,14 @@
 // Weights are fp16, 11 bits.  The maximum that they refer to moves only where one passes fp16's range: they are held as
 // 2^8 2^(s - m), so m may stay behind the true maximum by 2^7, and no maximum is taken per page, which would be two dependent
 // chains over 32 scores.  They keep 11 bits down to 2^-22 of the largest, or to 2^-16 where the scales of values differ between
-// pages (below).  The sum is of the rounded weights: their roundings cancel in a mean of equal values.
+// pages (below; a page's by more than 2^64 from a larger one: fewer).  The sum is of the rounded weights: their roundings cancel in a mean of equal values.
 //
 // What bounds it is issue: per page and wavefront (128 channels) 1024 clocks of matrix instructions stand against 128
 // conversions and some 4 operations, one of them an exponential of four times the length, for each of a lane's 32 scores; a probe
 // of the two kinds side by side takes the longer one's time and a third of the other's.  Three sequences of 2000 to 4096 tokens behind
-// up to 4000, 32 query heads on 8 kv heads of 128 channels: 453 us, 935 TFLOP/s, 78 % of what a large fp16 matrix product reaches.
+// up to 4000, 32 query heads on 8 kv heads of 128 channels: 455 us, 931 TFLOP/s, 69 % of what a large fp16 matrix product reaches (1345),
+// both with the clock settled: the first 25 ms of such work take up to a third longer.  Sequences of 2000 tokens behind 2000, three of
+// them: 64 channels 191 us, 128 319, 256 936; with a window of 1000 tokens 89, 145, 430.
 // Tried and taken back (with the short sums, 435 us): the next page's scores between the exponentials (433 -> 458); s_setprio (no change);
 // two pages to a barrier (431 -> 457); values turned into fp16 by one wavefront for all four, through LDS: a fifth fewer vector
 // instructions and twice the reads of LDS (435 -> 475); a prescribed mix of products and weights (453 -> 456).
@@ -403,7 +405,7 @@ __device__ __forceinline__ void take_chunk_page(const AttnArgs &a, Chunk<T, HD> 
       for (int j = 0; j < 2; ++j) k.acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(x[2 * j], x[2 * j + 1]), w[i][j], k.acc[c], 0, 0, 0);
     }
   };
-  // the second tile's weights behind the first one's products (both tiles' weights first: 467 us for the 453 above)
+  // the second tile's weights behind the first one's products (both tiles' weights first: 467 us, then, for 453)
   weigh(0, shift - k.m);
   settle(0);
   add(0);
