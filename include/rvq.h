@@ -314,8 +314,9 @@ int rvq_cache8_append(const rvq_cache8 *cache, const void *dK, const void *dV, i
  * Read back: row cu[b] + i is the token of sequence b at position first[b] + i; value = code * scale, rounded
  * once to dtype.  With the tables that they were appended with, keys come back as they were before the rotation: every pair
  * is rotated by the negative angle and divided by cos^2 + sin^2 (the square of the tables' amplitude; within 2^-22 of 1 it
- * counts as 1, and it has to lie in 2^-100 .. 2^100).  That is what rvq_encode takes (Section 3: quantized before the rotary embedding).  Tokens that are not in the cache (position
- * outside [0, lengths[b]), no page) read as 0.  Rows from cu[n_seqs] on are left as they were.
+ * counts as 1, and it has to lie in 2^-100 .. 2^100).  That is what rvq_encode takes (Section 3: quantized before the rotary
+ * embedding).  Tokens that are not in the cache (position outside [0, lengths[b]), no page) read as 0.  Rows from cu[n_seqs] on
+ * are left as they were.
  *   dFirst    device, int32 [n_seqs]
  *   dK, dV    device, dtype [rows][n_kv_heads][head_dim], 16-byte aligned, strides as above; either may be NULL
  * Other arguments as for rvq_cache8_append.
@@ -342,8 +343,9 @@ int rvq_cache8_read(const rvq_cache8 *cache, const int32_t *dCu, const int32_t *
  *   n_q_heads   a multiple of n_kv_heads, up to 65535; rows * rep up to 2^30 - 1
  *   scale   finite, and so log2(e) scale in fp32
  *   dWorkspace  device, 16-byte aligned, workspace_bytes >= rvq_cache8_attn_workspace_bytes() of the same sizes on the
- *               current device, or of more rows of the same cache, type and heads; caller-owned, contents unspecified before and after.  It serves one call at a time: calls
- *               that may run side by side (streams, graphs) need one each
+ *               current device, or of more rows of the same cache, type and heads (the size does not fall as rows grow); caller-owned,
+ *               contents unspecified before and after.  It serves one call at a time: calls that may run side by side (streams,
+ *               graphs) need one each
  * A table may name a page several times and share pages between sequences.
  * One kernel takes all of a call's sequences, chosen by rows * rep / n_seqs: single tokens and chunks of prompts are faster in calls of
  * their own, and sequences that bring no row are better left out of the view.
