@@ -66,7 +66,7 @@ def test_scales_that_fall_and_rise(gpu_device, dtype, columns, exps):
 
 
 @pytest.mark.parametrize("dtype,columns", [("fp32", (2, 3)), ("bf16", (2, 3)), ("bf16", (4, 80)), ("bf16", (4, 200))])
-@pytest.mark.parametrize("large,small", [(30, -20), (-20, 30), (0, -45), (-90, -40)])
+@pytest.mark.parametrize("large,small", [(30, -20), (-20, 30), (0, -45), (-90, -40), (32, -32), (-32, 32)])
 def test_rows_whose_windows_see_other_scales(gpu_device, dtype, columns, large, small):
     """Neighbouring rows share a block of columns: one sees a page of a scale that another's window hides, or that lies behind it."""
     exps = [large] + [small] * 3 + [large]
@@ -85,7 +85,7 @@ def test_values_near_the_end_of_fp32(gpu_device, dtype, columns, exps, code):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("hd,rot,layout", [(64, 32, o.HALVES), (128, 128, o.ADJACENT), (256, 64, o.ADJACENT), (256, 256, o.HALVES)])
-@pytest.mark.parametrize("amplitude", [1.2, 0.3, 1.0])
+@pytest.mark.parametrize("amplitude", [1.2, 0.3, 1.0, 2.0**-40, 2.0**45])
 def test_keys_come_back_from_tables_of_any_amplitude(gpu_device, dtype, hd, rot, layout, amplitude):
     """Appended and read with the same tables, as contexts that are stretched have them: the keys, but for their codes' rounding."""
     torch, b, rng = base._t(), base._b(), np.random.default_rng(hd + rot)
